@@ -416,6 +416,134 @@ av_status av_step_n_static(const av_config *cfg, int32_t num_rules, const int32_
                            void *state, const void *init, int32_t *counters, int32_t k,
                            const uint8_t *actions, float *rewards, uint8_t *done);
 
+/* ---------------------------------------------------------------------------------------
+ * The learner's side of a rollout (paper Sec. 2.3: agents are trained on what the stepped
+ * environments return).  The operators read and write the rollout's own device buffers,
+ * [T][B] with T steps of B environments: rewards and done flags from av_step_n, actions for
+ * av_step, and an agent's values and logits over them.  They need no batch, keep nothing
+ * between calls, allocate nothing, and run on `stream` of `device` (the calling thread's
+ * current device is left as it was); asynchronous, and capturable into a HIP graph.  Equal
+ * calls give equal bits.
+ * ------------------------------------------------------------------------------------- */
+
+/* Element types of the operators' tensors.  Arithmetic, states and sums are held in 32 bits (or
+ * 64 where stated); a value of a 16-bit type is rounded once, when it is stored. */
+typedef enum { AV_F32 = 0, AV_F16 = 1, AV_BF16 = 2 } av_dtype;
+
+/* Types of given tokens: actions as av_step takes them, or wider token numbers. */
+typedef enum { AV_IDS_U8 = 0, AV_IDS_I32 = 1, AV_IDS_I64 = 2 } av_ids_type;
+
+typedef enum {
+    AV_SCAN_LINEAR = 0,   /* s_t = a_t s_{t-1} + x_t, a_t = gate */
+    AV_SCAN_GATED = 1     /* s_t = a_t s_{t-1} + (1 - a_t) x_t, a_t = 1 / (1 + exp(-gate)) */
+} av_scan_form;
+
+/* Shape and layout of a recurrence: `rows` sequences of `steps` steps and `width` values.
+ * Element (t, b, d) of a tensor is at t * its step stride + b * its row stride + d (in elements;
+ * the width is contiguous).  Inputs may have strides of 0 (a broadcast input). */
+typedef struct {
+    int64_t steps;            /* T in [0, 2^31) */
+    int64_t rows, width;      /* B >= 0, D >= 1, B x D < 2^31 */
+    int32_t dtype;            /* av_dtype of x, gate, y and their gradients */
+    int32_t form;             /* av_scan_form */
+    int32_t reverse;          /* 0: t runs 0 .. T-1; 1: T-1 .. 0 ("t - 1" below is then t + 1) */
+    int32_t gate_per_value;   /* 0: gate [T][B][D]; 1: gate [D], the same at every t and b (its
+                                 strides are not used) */
+    int64_t x_step, x_row, gate_step, gate_row, y_step, y_row;
+    int64_t cut_step, cut_row;
+    int64_t dy_step, dy_row, dx_step, dx_row, dgate_step, dgate_row;  /* av_scan_backward */
+    int32_t device, reserved;
+    void *stream;             /* hipStream_t; NULL = null stream */
+} av_scan_config;
+
+/* Bytes of device memory (*bytes, may be 0) that av_scan, or av_scan_backward with backward != 0,
+ * uses as workspace for these sizes on this device.  Host only. */
+av_status av_scan_workspace(const av_scan_config *cfg, int32_t backward, size_t *bytes);
+
+/* A gated linear recurrence over a rollout, with s_{-1} = h0 (0 where NULL):
+ *   y[t] = s_t;  a step whose cut flag is set starts anew: the state coming in is dropped
+ *   (whatever it is, NaN included) and s_t = x_t, or (1 - a_t) x_t.
+ * Reversed, with the rollout's done flags as cut, this is the discounted return
+ * y[t] = x[t] + gamma (1 - done[t]) y[t+1] (gate the single value gamma), or the advantage when x
+ * is the temporal-difference error.  Forward, with the done flags of the step before as cut, it
+ * is a recurrent agent's memory that starts anew with every episode; T = 1 is its acting step.
+ *   x, gate   device, dtype;  cut device uint8 [T][B] or NULL (never)
+ *   h0, last  device float [B][D] or NULL: the state before the first step and after the last
+ *             processed one (T = 0: h0).  They may be the same buffer.
+ *   y         device, dtype; may be x itself (the same pointer and strides)
+ * Products of gates are formed over spans of steps: gates are decays, |a| <= 1 (larger ones work
+ * while their product over any span is finite in 32 bits).  A state that is not finite leaves every
+ * later output of its column not finite until the next cut.
+ * workspace: av_scan_workspace bytes or more, 16-byte aligned, not shared by calls that may
+ * overlap (two graphs, two streams); NULL where that is 0.  AV_EINVAL, before any device work, for
+ * NULL pointers, sizes or types out of range, an output stride that makes its elements
+ * overlap, a workspace too small. */
+av_status av_scan(const av_scan_config *cfg, const void *x, const void *gate, const uint8_t *cut,
+                  const float *h0, void *y, float *last, void *workspace,
+                  size_t workspace_bytes);
+
+/* Gradients of av_scan.  dy: the gradient of y (device, dtype); dlast: of last (device float
+ * [B][D]) or NULL (0).  y is the output of av_scan, which stands for the states (with a 16-bit
+ * type dgate sees them rounded to it).  Outputs: dx (dtype), dgate (dtype; [T][B][D], or [D]
+ * summed in 32 bits over T and B, in a fixed order) or NULL if not wanted, dh0 (device float [B][D])
+ * or NULL.  x may be NULL in the linear form, which does not read it.  dx may be dy, and dgate
+ * [T][B][D] may be gate (the same pointer and strides); no other output may overlap an input.
+ * Workspace and errors as av_scan, with av_scan_workspace(cfg, 1, ...). */
+av_status av_scan_backward(const av_scan_config *cfg, const void *x, const void *gate,
+                           const uint8_t *cut, const float *h0, const void *y, const void *dy,
+                           const float *dlast, void *dx, void *dgate, float *dh0,
+                           void *workspace, size_t workspace_bytes);
+
+/* Distributions over choices: `rows` rows of `choices` logits, row r at r * row_stride elements. */
+typedef struct {
+    int64_t rows;             /* N in [0, 2^31) */
+    int64_t choices;          /* A in [1, 2^31 - 1025] */
+    int32_t dtype;            /* av_dtype of the logits and their gradient */
+    int32_t ids_type;         /* av_ids_type */
+    int64_t row_stride;       /* of the logits, in elements (0: one row for all) */
+    int64_t drow_stride;      /* of dlogits (av_log_probs_backward) */
+    int32_t top;              /* alternatives per row, in [0, AV_TOP_MAX] */
+    int32_t device;
+    void *stream;             /* hipStream_t; NULL = null stream */
+} av_tokens_config;
+#define AV_TOP_MAX 32
+
+/* Log-probabilities of given tokens under softmax(logits), the entropy, and the most likely
+ * alternatives (policy gradients, behaviour cloning and scoring, paper Sec. 2.3).
+ *   ids       device [N] (ids_type) or NULL with logp NULL.  A number outside [0, A) is padding:
+ *             its logp is 0 and it passes no gradient to the logits.
+ *   logp      device float [N] or NULL
+ *   entropy   device float [N] or NULL, in nats
+ *   stats     device float [N][2] or NULL: the row's normaliser as av_log_probs_backward takes it
+ *   top_logp, top_ids   device float / int32 [N][top], log-probability falling, of equal ones
+ *             the lowest index first; with top = 0 not used, else neither may be NULL.
+ * A logit of -infinity is a masked choice: probability 0, no part in entropy or alternatives
+ * (places left over get id -1 and -infinity).  A row without any other has logp -infinity,
+ * entropy 0.  A row holding a NaN or +infinity has NaN results and ids -1. */
+av_status av_log_probs(const av_tokens_config *cfg, const void *logits, const void *ids,
+                       float *logp, float *entropy, float *stats, float *top_logp,
+                       int32_t *top_ids);
+
+/* Gradient of av_log_probs: with p = softmax(logits) and the entropy H,
+ *   dlogits_i = dlogp ([i = id] - p_i) - dentropy p_i (log p_i + H)
+ * (a p_i below 2^-126 counts as 0).
+ * stats and entropy as av_log_probs stored them for the same logits; dlogp, dentropy device float
+ * [N], either may be NULL (0; entropy is read only with dentropy, ids only with dlogp).  dlogits:
+ * device, dtype, row r at r * drow_stride; may be the logits themselves (the same pointer and
+ * stride).  Masked choices and rows without any choice get 0; a row with NaN results gets NaN. */
+av_status av_log_probs_backward(const av_tokens_config *cfg, const void *logits, const void *ids,
+                                const float *stats, const float *entropy, const float *dlogp,
+                                const float *dentropy, void *dlogits);
+
+/* Draw one action per row from softmax(logits), for av_step: the smallest i for which
+ * p_0 + .. + p_i > u, in 64 bits; the last choice that is not masked if there is none (u >= 1 or
+ * NaN).  uniform: device float [N], numbers in [0, 1) from the caller's generator; actions:
+ * device uint8 [N]; logp: device float [N] or NULL, the drawn action's log-probability.
+ * A <= 256 (an action is one byte).  A row without any choice draws 0 with logp -infinity, a row
+ * holding a NaN or +infinity draws 0 with logp NaN. */
+av_status av_draw_actions(const av_tokens_config *cfg, const void *logits, const float *uniform,
+                          uint8_t *actions, float *logp);
+
 /* Device pointer to the packed current maps, owned by the batch and valid until the
  * next av_reset / av_set_state / av_destroy_batch.  Layout: rows of row_bytes bytes,
  * index [c][env][y] (channel-major over the whole batch); cell (env, c, y, x) is bit x

@@ -26,6 +26,11 @@ ENGINE_NAMES = {v: k for k, v in ENGINES.items()}
 AV_RULES_PARALLEL, AV_RULES_SEQUENTIAL = 0, 1
 RULE_MODES = {"parallel": AV_RULES_PARALLEL, "sequential": AV_RULES_SEQUENTIAL}
 AV_SITES_ROW_MAJOR, AV_SITES_RANDOM = 0, 1
+AV_F32, AV_F16, AV_BF16 = 0, 1, 2
+AV_IDS_U8, AV_IDS_I32, AV_IDS_I64 = 0, 1, 2
+AV_SCAN_LINEAR, AV_SCAN_GATED = 0, 1
+SCAN_FORMS = {"linear": AV_SCAN_LINEAR, "gated": AV_SCAN_GATED}
+AV_TOP_MAX = 32
 SITE_ORDERS = {"rowmajor": AV_SITES_ROW_MAJOR, "random": AV_SITES_RANDOM}
 
 # Every symbol include/autoverse.h declares.
@@ -35,7 +40,8 @@ ABI_SYMBOLS = ("av_create_batch", "av_load_rules", "av_set_rule_control", "av_re
                "av_get_state", "av_set_state", "av_set_stream", "av_destroy_batch",
                "av_mutate_maps", "av_mutate_rules", "av_search_create", "av_search_load_rules",
                "av_search_begin", "av_search_expand", "av_search_frontier", "av_search_destroy",
-               "av_step_n_static", "av_last_error")
+               "av_step_n_static", "av_scan_workspace", "av_scan", "av_scan_backward",
+               "av_log_probs", "av_log_probs_backward", "av_draw_actions", "av_last_error")
 
 
 class av_config(ctypes.Structure):
@@ -91,6 +97,25 @@ class av_info(ctypes.Structure):
                 ("state_bytes", ctypes.c_size_t), ("blob_bytes", ctypes.c_size_t)]
 
 
+class av_scan_config(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("steps", "rows", "width")]
+                + [(n, ctypes.c_int32) for n in ("dtype", "form", "reverse", "gate_per_value")]
+                + [(n, ctypes.c_int64) for n in (
+                    "x_step", "x_row", "gate_step", "gate_row", "y_step", "y_row", "cut_step",
+                    "cut_row", "dy_step", "dy_row", "dx_step", "dx_row", "dgate_step",
+                    "dgate_row")]
+                + [("device", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                   ("stream", ctypes.c_void_p)])
+
+
+class av_tokens_config(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("choices", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("ids_type", ctypes.c_int32),
+                ("row_stride", ctypes.c_int64), ("drow_stride", ctypes.c_int64),
+                ("top", ctypes.c_int32), ("device", ctypes.c_int32),
+                ("stream", ctypes.c_void_p)]
+
+
 class AvError(RuntimeError):
     def __init__(self, fn: str, status: int, message: str):
         super().__init__(f"{fn}: status {status}: {message}")
@@ -140,6 +165,12 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "av_search_destroy": ([P], ctypes.c_int),
         "av_step_n_static": ([ctypes.POINTER(av_config), I32, P, P, P, P, P, P, P, I32, P, P, P],
                              ctypes.c_int),
+        "av_scan_workspace": ([P, I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "av_scan": ([P] * 8 + [SZ], ctypes.c_int),
+        "av_scan_backward": ([P] * 12 + [SZ], ctypes.c_int),
+        "av_log_probs": ([P] * 8, ctypes.c_int),
+        "av_log_probs_backward": ([P] * 8, ctypes.c_int),
+        "av_draw_actions": ([P] * 5, ctypes.c_int),
         "av_last_error": ([], ctypes.c_char_p),
     }
     for name, (args, res) in sig.items():
@@ -404,6 +435,229 @@ def av_destroy_batch(batch):
     _check("av_destroy_batch", load_library().av_destroy_batch(batch))
 
 
+# --- the learner's operators ----------------------------------------------------------------
+
+_dtypes = None
+
+
+def _types():
+    """torch's element types and token types as the library numbers them."""
+    global _dtypes
+    if _dtypes is None:
+        torch = _torch()
+        _dtypes = ({torch.float32: AV_F32, torch.float16: AV_F16, torch.bfloat16: AV_BF16},
+                   {torch.uint8: AV_IDS_U8, torch.int32: AV_IDS_I32, torch.int64: AV_IDS_I64},
+                   torch)
+    return _dtypes
+
+
+def _operand(t, name, dtype, shape, device):
+    """The address of a device tensor of this type, shape and device whose last dimension is
+    contiguous, and its strides; (None, ...) of none."""
+    if t is None:
+        return None, (0,) * len(shape)
+    if not isinstance(t, _types()[2].Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr(), strides
+
+
+def _packed(t, name, dtype, shape, device):
+    """The address of a contiguous device tensor of this type, shape and device, or None."""
+    if t is None:
+        return None
+    p, _ = _operand(t, name, dtype, shape, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return p
+
+
+def _scan_config(x, gate, cut, form, reverse):
+    floats, _, torch = _types()
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in floats:
+        raise TypeError("x must be a float32, float16 or bfloat16 device tensor [T][B][D]")
+    shape, device, dtype = x.shape, x.device, x.dtype
+    T, B, D = shape
+    if B == 0 or D == 0:
+        raise ValueError(f"an empty recurrence: x has shape {tuple(shape)}")
+    c = av_scan_config()
+    c.steps, c.rows, c.width, c.dtype = T, B, D, floats[dtype]
+    c.form = SCAN_FORMS[form] if isinstance(form, str) else int(form)
+    c.reverse = 1 if reverse else 0
+    px, s = _operand(x, "x", dtype, shape, device)
+    c.x_step, c.x_row = s[0], s[1]
+    if gate.dim() == 1:
+        c.gate_per_value = 1
+        pg, _ = _operand(gate, "gate", dtype, shape[2:], device)
+    else:
+        pg, s = _operand(gate, "gate", dtype, shape, device)
+        c.gate_step, c.gate_row = s[0], s[1]
+    pc = None
+    if cut is not None:
+        if not isinstance(cut, torch.Tensor) or not cut.is_cuda:
+            raise TypeError("cut must be a device tensor")
+        if cut.dtype != torch.uint8 or cut.shape != shape[:2] or cut.device != device:
+            raise ValueError(f"cut must be a uint8 tensor of shape {tuple(shape[:2])} on {device}")
+        pc = cut.data_ptr()
+        c.cut_step, c.cut_row = cut.stride()
+    c.device = device.index
+    c.stream = torch.cuda.current_stream(device).cuda_stream
+    return c, px, pg, pc
+
+
+def av_scan_workspace(steps, rows, width, gate_per_value=False, backward=False) -> int:
+    """Bytes of workspace av_scan (or av_scan_backward) uses for these sizes."""
+    c = av_scan_config()
+    c.steps, c.rows, c.width, c.gate_per_value = steps, rows, width, int(bool(gate_per_value))
+    n = ctypes.c_size_t(0)
+    _check("av_scan_workspace", load_library().av_scan_workspace(
+        ctypes.byref(c), int(bool(backward)), ctypes.byref(n)))
+    return n.value
+
+
+def _workspace(lib, c, ref, backward, workspace, device):
+    """The workspace's tensor (kept alive by the caller), address and size: the caller's, or a
+    new one from torch's allocator on the current stream."""
+    torch = _types()[2]
+    if workspace is None:
+        n = ctypes.c_size_t(0)
+        _check("av_scan_workspace", lib.av_scan_workspace(ref, backward, ctypes.byref(n)))
+        if n.value == 0:
+            return None, None, 0
+        workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or \
+            workspace.device != device:
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
+    return workspace, workspace.data_ptr(), workspace.numel()
+
+
+def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=False,
+            workspace=None):
+    """Gated linear recurrence over time.  x, y: device tensors [T][B][D] of one floating type;
+    gate the same, or [D]; h0, last: float32 [B][D] or None; cut: uint8 [T][B] or None (a step
+    whose flag is set starts anew).  y may be x.  Runs on the current stream of x's device."""
+    lib = load_library()
+    c, px, pg, pc = _scan_config(x, gate, cut, form, reverse)
+    shape, device = x.shape, x.device
+    py, s = _operand(y, "y", x.dtype, shape, device)
+    c.y_step, c.y_row = s[0], s[1]
+    f32 = _types()[2].float32
+    ph = _packed(h0, "h0", f32, shape[1:], device)
+    pl = _packed(last, "last", f32, shape[1:], device)
+    ref = ctypes.byref(c)
+    keep, pw, n = _workspace(lib, c, ref, 0, workspace, device)
+    rc = lib.av_scan(ref, px, pg, pc, ph, py, pl, pw, n)
+    if rc:
+        _check("av_scan", rc)
+
+
+def av_scan_backward(x, gate, y, dy, dx, dgate=None, h0=None, dlast=None, dh0=None, cut=None,
+                     form="linear", reverse=False, workspace=None):
+    """Gradients of av_scan, called as it was: y its output, dy and dlast the gradients of y and
+    last; dx, dgate (like gate, or None) and dh0 (float32 [B][D], or None) are written."""
+    lib = load_library()
+    c, px, pg, pc = _scan_config(x, gate, cut, form, reverse)
+    shape, device, dtype = x.shape, x.device, x.dtype
+    py, s = _operand(y, "y", dtype, shape, device)
+    c.y_step, c.y_row = s[0], s[1]
+    pdy, s = _operand(dy, "dy", dtype, shape, device)
+    c.dy_step, c.dy_row = s[0], s[1]
+    pdx, s = _operand(dx, "dx", dtype, shape, device)
+    c.dx_step, c.dx_row = s[0], s[1]
+    if c.gate_per_value:
+        pdg = _packed(dgate, "dgate", dtype, shape[2:], device)
+    else:
+        pdg, s = _operand(dgate, "dgate", dtype, shape, device)
+        c.dgate_step, c.dgate_row = s[0], s[1]
+    f32 = _types()[2].float32
+    ph = _packed(h0, "h0", f32, shape[1:], device)
+    pdl = _packed(dlast, "dlast", f32, shape[1:], device)
+    pdh = _packed(dh0, "dh0", f32, shape[1:], device)
+    ref = ctypes.byref(c)
+    keep, pw, n = _workspace(lib, c, ref, 1, workspace, device)
+    rc = lib.av_scan_backward(ref, px, pg, pc, ph, py, pdy, pdl, pdx, pdg, pdh, pw, n)
+    if rc:
+        _check("av_scan_backward", rc)
+
+
+def _tokens_config(logits, ids):
+    floats, whole, torch = _types()
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() != 2 or \
+            logits.dtype not in floats:
+        raise TypeError("logits must be a float32, float16 or bfloat16 device tensor [N][A]")
+    shape, device = logits.shape, logits.device
+    pl, s = _operand(logits, "logits", logits.dtype, shape, device)
+    c = av_tokens_config()
+    c.rows, c.choices, c.dtype, c.row_stride = shape[0], shape[1], floats[logits.dtype], s[0]
+    pi = None
+    if ids is not None:
+        if not isinstance(ids, torch.Tensor) or ids.dtype not in whole:
+            raise TypeError("ids must be a uint8, int32 or int64 device tensor [N]")
+        c.ids_type = whole[ids.dtype]
+        pi = _packed(ids, "ids", ids.dtype, shape[:1], device)
+    c.device = device.index
+    c.stream = torch.cuda.current_stream(device).cuda_stream
+    return c, pl, pi
+
+
+def av_log_probs(logits, ids=None, logp=None, entropy=None, stats=None, top_logp=None,
+                 top_ids=None):
+    """Log-probabilities of the given tokens.  logits: device tensor [N][A]; ids: uint8, int32 or
+    int64 [N] (outside [0, A): padding); logp, entropy: float32 [N]; stats: float32 [N][2], for
+    av_log_probs_backward; top_logp, top_ids: float32 / int32 [N][k], the k <= 32 most likely.
+    What is None is not written.  Runs on the current stream of the logits' device."""
+    c, pl, pi = _tokens_config(logits, ids)
+    torch, device, N = _types()[2], logits.device, logits.shape[0]
+    f32 = torch.float32
+    row = logits.shape[:1]
+    p = [_packed(logp, "logp", f32, row, device), _packed(entropy, "entropy", f32, row, device),
+         _packed(stats, "stats", f32, (N, 2), device)]
+    if top_logp is not None or top_ids is not None:
+        if top_logp is None or top_ids is None or top_logp.dim() != 2:
+            raise ValueError("top_logp and top_ids [N][k] go together")
+        c.top = top_logp.shape[1]
+        p += [_packed(top_logp, "top_logp", f32, (N, c.top), device),
+              _packed(top_ids, "top_ids", torch.int32, (N, c.top), device)]
+    else:
+        p += [None, None]
+    rc = load_library().av_log_probs(ctypes.byref(c), pl, pi, *p)
+    if rc:
+        _check("av_log_probs", rc)
+
+
+def av_log_probs_backward(logits, ids, stats, entropy, dlogp, dentropy, dlogits):
+    """Gradient of av_log_probs: stats and entropy as it stored them, dlogp and dentropy float32
+    [N] or None (then ids, or entropy, may be None too), dlogits like logits; it may be logits."""
+    c, pl, pi = _tokens_config(logits, ids)
+    f32, device, row = _types()[2].float32, logits.device, logits.shape[:1]
+    pd, s = _operand(dlogits, "dlogits", logits.dtype, logits.shape, device)
+    c.drow_stride = s[0]
+    rc = load_library().av_log_probs_backward(
+        ctypes.byref(c), pl, pi, _packed(stats, "stats", f32, (row[0], 2), device),
+        _packed(entropy, "entropy", f32, row, device), _packed(dlogp, "dlogp", f32, row, device),
+        _packed(dentropy, "dentropy", f32, row, device), pd)
+    if rc:
+        _check("av_log_probs_backward", rc)
+
+
+def av_draw_actions(logits, uniform, actions, logp=None):
+    """Draw an action per row of logits [N][A], A <= 256: uniform float32 [N] in [0, 1), actions
+    uint8 [N], logp float32 [N] or None."""
+    c, pl, _ = _tokens_config(logits, None)
+    torch, device, row = _types()[2], logits.device, logits.shape[:1]
+    rc = load_library().av_draw_actions(
+        ctypes.byref(c), pl, _packed(uniform, "uniform", torch.float32, row, device),
+        _packed(actions, "actions", torch.uint8, row, device),
+        _packed(logp, "logp", torch.float32, row, device))
+    if rc:
+        _check("av_draw_actions", rc)
+
+
 class Batch:
     """A batch of B environments on one GPU, with reusable device buffers for actions,
     rewards and done flags."""
@@ -478,6 +732,35 @@ class Batch:
             obs = torch.empty((self.B, self.C, w, w), dtype=torch.uint8, device=self.device)
         av_step_observe(self.h, k, actions, rewards, done, w, obs)
         return rewards, done, obs
+
+    def act(self, logits, uniform, actions=None, logp=None):
+        """Draw every environment's action for the next step: logits [B][A] and uniform numbers
+        float32 [B] on the device; returns (actions uint8 [B], their log-probabilities [B])."""
+        torch = _torch()
+        if tuple(logits.shape[:1]) != (self.B,):
+            raise ValueError(f"logits must have {self.B} rows, got {tuple(logits.shape)}")
+        if actions is None:
+            actions = torch.empty(self.B, dtype=torch.uint8, device=self.device)
+        if logp is None:
+            logp = torch.empty(self.B, dtype=torch.float32, device=self.device)
+        av_draw_actions(logits, uniform, actions, logp)
+        return actions, logp
+
+    def returns(self, rewards, done, gamma, after=None, out=None):
+        """Discounted returns of a rollout: rewards float32 [k][B] (or temporal-difference errors,
+        for advantages) and done [k][B] as step_n gives them, gamma a number or a float32 device
+        tensor [1], after float32 [B] the value of what follows the last step (or None); returns
+        out [k][B], out[t] = rewards[t] + gamma (1 - done[t]) out[t + 1]."""
+        torch = _torch()
+        if rewards.dim() != 2 or rewards.shape[1] != self.B:
+            raise ValueError(f"rewards must be [k][{self.B}], got {tuple(rewards.shape)}")
+        if not isinstance(gamma, torch.Tensor):
+            gamma = torch.full((1,), gamma, dtype=torch.float32, device=self.device)
+        if out is None:
+            out = torch.empty_like(rewards)
+        av_scan(rewards[:, :, None], gamma, out[:, :, None],
+                h0=None if after is None else after[:, None], cut=done, reverse=True)
+        return out
 
     def maps(self, out=None):
         torch = _torch()

@@ -297,6 +297,50 @@ void compile_group_tables(const GenericProgram &p, int H, int W, int C, int list
                           std::vector<uint32_t> &tab, int &stride, int &entry_words);
 hipError_t launch_group_step(const StepArgs &a, hipStream_t s);
 
+// The learner's operators (av_learn.cpp checks the arguments, k_scan.hip and k_tokens.hip run).
+//
+// A recurrence in processing order: every tensor points at the first processed step and its step
+// stride carries the sign of the order; the gradient is processed from the last step to the
+// first.  first / final: the state (or its gradient) before the first processed step and after
+// the last one.
+constexpr int kScanSteps = 8;         // consecutive steps a wave holds in registers
+struct ScanArgs {
+    int64_t T, N, D, chunk;           // steps, columns B x D, width, steps per chunk
+    const void *x, *gate, *y, *dy;
+    const uint8_t *cut;
+    const float *first, *h0;          // h0: the state itself, which the gradient of a gate needs
+    float *final;
+    void *out, *dgate;                // y, or dx; and the gradient of the gates
+    float *part;                      // a gate per value: the workgroups' sums
+    void *slots;                      // chunks > 1: [chunks][N] spans
+    int64_t x_step, x_row, gate_step, gate_row, y_step, y_row, dy_step, dy_row, out_step, out_row,
+        dgate_step, dgate_row, cut_step, cut_row;
+};
+struct ScanPlan {
+    int vec, waves, chunks, runs;     // columns a lane, waves a workgroup, chunks of time, and
+                                      // runs of rows in the first sum of a gate per value
+    int64_t chunk;                    // steps
+    size_t part_off, bytes;           // workspace: slots, then the sums
+};
+ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, bool pairs, bool col, bool back);
+hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool gated, bool col,
+                       bool back, hipStream_t s);
+
+struct TokenArgs {
+    int64_t N, stride, dstride;       // rows, and the rows' strides in elements
+    int A, top, ids_type;
+    const void *logits, *ids;
+    float *logp, *entropy, *stats, *top_logp;
+    int32_t *top_ids;
+    const float *in_stats, *in_entropy, *dlogp, *dentropy;   // the gradient's inputs
+    void *dlogits;
+    const float *uniform;
+    uint8_t *actions;
+};
+hipError_t launch_log_probs(const TokenArgs &a, int dtype, hipStream_t s);
+hipError_t launch_log_probs_backward(const TokenArgs &a, int dtype, hipStream_t s);
+hipError_t launch_draw(const TokenArgs &a, int dtype, hipStream_t s);
+
 // Wave slots of the current device (8 waves per SIMD, 4 SIMDs per CU; 0 if it cannot be
 // asked): the most waves resident at once.
 long long device_wave_slots();

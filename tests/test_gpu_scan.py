@@ -1,0 +1,307 @@
+"""av_scan and av_scan_backward on the GPU against the recurrence written out in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import learn_ref as ref
+import paper_2407_04221_amd as av
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def make(shape, dtype, r, scale=1.0, mean=0.0, layout="time", pad=0, shift=0):
+    """A device tensor [T][B][D] of normal numbers in the given memory order, with `pad` elements
+    between rows and `shift` before the first, and its values in 64 bits."""
+    T, B, D = shape
+    v = torch.from_numpy(r.normal(size=shape) * scale + mean).to(TYPES[dtype])
+    dims = (T, B) if layout == "time" else (B, T)
+    flat = torch.full((shift + dims[0] * dims[1] * (D + pad),), 7.0, dtype=TYPES[dtype],
+                      device="cuda")
+    t = flat[shift:].view(dims[0], dims[1], D + pad)[:, :, :D]
+    if layout != "time":
+        t = t.transpose(0, 1)
+    t.copy_(v)
+    return t, v.double().numpy()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def run(T, B, D, dtype="f32", form="linear", reverse=False, columns=False, cut=0.1, state=True,
+        train=True, layout="time", pad=0, shift=0, seed=0, mean=None):
+    r = np.random.default_rng(seed)
+    kw = dict(layout=layout, pad=pad, shift=shift)
+    x, x64 = make((T, B, D), dtype, r, **kw)
+    if mean is None:
+        mean = 2.0 if form == "gated" else 0.0
+    if columns:
+        g64 = r.normal(size=D) + mean if form == "gated" else r.uniform(-1, 1, size=D)
+        gate = torch.from_numpy(g64).to(TYPES[dtype]).cuda()
+        g64 = host(gate)
+    elif form == "gated":
+        gate, g64 = make((T, B, D), dtype, r, mean=mean, **kw)
+    else:
+        gate, _ = make((T, B, D), dtype, r, **kw)
+        gate.copy_(torch.from_numpy(r.uniform(-1, 1, size=(T, B, D))))
+        g64 = host(gate)
+    c64 = (r.random((T, B)) < cut).astype(np.uint8) if cut is not None else None
+    c = torch.from_numpy(c64 * 200).to(torch.uint8).cuda() if cut is not None else None
+    h0 = torch.randn((B, D), device="cuda") if state else None
+    h64 = host(h0) if state else None
+    y, _ = make((T, B, D), dtype, r, **kw)
+    last = torch.empty((B, D), device="cuda") if state else None
+    av.av_scan(x, gate, y, h0=h0, last=last, cut=c, form=form, reverse=reverse)
+    got = {"y": y}
+    if state:
+        got["last"] = last
+    dy64 = dl64 = None
+    if train:
+        dy, dy64 = make((T, B, D), dtype, r, **kw)
+        dlast = torch.randn((B, D), device="cuda") if state else None
+        dl64 = host(dlast) if state else None
+        dx, _ = make((T, B, D), dtype, r, **kw)
+        dgate = torch.empty_like(gate) if columns else make((T, B, D), dtype, r, **kw)[0]
+        dh0 = torch.empty((B, D), device="cuda") if state else None
+        av.av_scan_backward(x, gate, y, dy, dx, dgate, h0=h0, dlast=dlast, dh0=dh0, cut=c,
+                            form=form, reverse=reverse)
+        got.update(dx=dx, dgate=dgate)
+        if state:
+            got["dh0"] = dh0
+    want = ref.scan(x64, g64, h64, c64, form, reverse, dy64, dl64, dtype)
+    for name, t in got.items():
+        ref.check(host(t), want[name], f"{name} (T {T}, B {B}, D {D})",
+                  dtype if name in ("y", "dx", "dgate") else "f32")
+
+
+@pytest.mark.parametrize("form", ["linear", "gated"])
+@pytest.mark.parametrize("T", [1, 2, 7, 8, 9, 63, 64, 65, 130, 517])
+def test_lengths(T, form):
+    run(T, 3, 5, form=form)
+    run(T, 2, 64, form=form, reverse=True, dtype="bf16")
+
+
+@pytest.mark.parametrize("B,D", [(1, 1), (1, 63), (1, 64), (1, 65), (2, 127), (64, 1), (130, 1),
+                                 (3, 128), (7, 130), (1, 257), (33, 2), (129, 6)])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_widths(B, D, dtype):
+    run(21, B, D, dtype=dtype, form="gated")
+    run(70, B, D, dtype=dtype, reverse=True, columns=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("form", ["linear", "gated"])
+@pytest.mark.parametrize("columns", [False, True])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_long_few_columns(dtype, form, columns, reverse):
+    """Time is cut into chunks here."""
+    run(5003, 1, 6, dtype=dtype, form=form, columns=columns, reverse=reverse, cut=0.003)
+    run(2048, 2, 65, dtype=dtype, form=form, columns=columns, reverse=reverse, cut=None)
+
+
+@pytest.mark.parametrize("pad,shift", [(0, 0), (2, 0), (1, 0), (0, 1), (8, 8), (3, 5)])
+@pytest.mark.parametrize("layout", ["time", "batch"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layouts(pad, shift, layout, dtype):
+    for T, B, D in ((19, 4, 12), (300, 3, 1)):
+        run(T, B, D, dtype=dtype, form="gated", layout=layout, pad=pad, shift=shift)
+        run(T, B, D, dtype=dtype, layout=layout, pad=pad, shift=shift, columns=True, reverse=True)
+
+
+def test_no_flags_and_no_state():
+    for kw in (dict(cut=None), dict(state=False), dict(cut=None, state=False), dict(cut=1.0)):
+        run(33, 5, 10, **kw)
+        run(33, 5, 10, form="gated", reverse=True, columns=True, **kw)
+
+
+def test_many_rows_of_a_shared_gate():
+    """Enough rows that the sum of the gate's gradient takes two steps."""
+    run(9, 5000, 2, columns=True)
+    run(40, 700, 16, columns=True, form="gated", dtype="bf16")
+
+
+def test_rows_between_are_left_alone():
+    r = np.random.default_rng(1)
+    x, _ = make((5, 3, 6), "f32", r)
+    wide = torch.full((5, 3, 9), 42.0, device="cuda")
+    av.av_scan(x, x * 0.1, wide[:, :, :6])
+    assert (wide[:, :, 6:] == 42.0).all() and (wide[:, :, :6] != 42.0).all()
+
+
+def test_a_cut_drops_whatever_comes_in():
+    """NaN and infinity before a cut do not pass it, in one tile, across tiles and chunks."""
+    for T, at in ((6, 3), (300, 200), (9000, 7001)):
+        x = torch.ones((T, 1, 2), device="cuda")
+        x[at - 2, 0, 0] = float("nan")
+        x[at - 2, 0, 1] = float("inf")
+        gate = torch.full((2,), 0.5, device="cuda")
+        cut = torch.zeros((T, 1), dtype=torch.uint8, device="cuda")
+        cut[at] = 1
+        y, last = torch.empty_like(x), torch.empty((1, 2), device="cuda")
+        h0 = torch.zeros((1, 2), device="cuda")
+        av.av_scan(x, gate, y, h0=h0, last=last, cut=cut)
+        fine = torch.isfinite(y)
+        assert fine[:at - 2].all() and fine[at:].all() and not fine[at - 2:at].any()
+        assert (y[at] == 1.0).all() and torch.isfinite(last).all()
+        h0[:] = float("nan")
+        cut[0] = 1
+        x[at - 2] = 1.0
+        av.av_scan(x, gate, y, h0=h0, last=last, cut=cut)
+        assert torch.isfinite(y).all() and (y[0] == 1.0).all()
+
+
+def test_gates_of_zero_and_one():
+    """A gate of 1 sums, a gate of 0 forgets; whole numbers come out exactly."""
+    T = 4000
+    x = torch.randint(-3, 4, (T, 1, 3), device="cuda").float()
+    gate = torch.ones((T, 1, 3), device="cuda")
+    gate[::17, 0, 1] = 0.0
+    gate[:, 0, 2] = -1.0
+    y = torch.empty_like(x)
+    av.av_scan(x, gate, y)
+    s = np.zeros(3)
+    want = []
+    xs, gs = host(x)[:, 0], host(gate)[:, 0]
+    for t in range(T):
+        s = gs[t] * s + xs[t]
+        want.append(s)
+    assert np.array_equal(host(y)[:, 0], np.array(want))
+
+
+def test_in_place_and_state_in_place():
+    r = np.random.default_rng(2)
+    for T, B, D in ((1, 300, 64), (50, 3, 10), (6000, 1, 4)):
+        x, _ = make((T, B, D), "f32", r)
+        gate = torch.rand((T, B, D), device="cuda")
+        h = torch.randn((B, D), device="cuda")
+        y, last = torch.empty_like(x), torch.empty_like(h)
+        av.av_scan(x, gate, y, h0=h, last=last)
+        z, state = x.clone(), h.clone()
+        av.av_scan(z, gate, z, h0=state, last=state)
+        assert torch.equal(z, y) and torch.equal(state, last)
+        dy = torch.randn((T, B, D), device="cuda")
+        dx, dgate = torch.empty_like(x), torch.empty_like(x)
+        av.av_scan_backward(x, gate, y, dy, dx, dgate, h0=h)
+        d, g = dy.clone(), gate.clone()
+        av.av_scan_backward(x, g, y, d, d, g, h0=h)
+        assert torch.equal(d, dx) and torch.equal(g, dgate)
+
+
+def test_broadcast_inputs():
+    """Strides of 0: the gradient of a sum, one gate for all steps."""
+    T, B, D = 40, 3, 8
+    x = torch.randn((T, B, D), device="cuda")
+    gate = torch.rand((1, B, D), device="cuda").expand(T, B, D)
+    dy = torch.ones((1, 1, D), device="cuda").expand(T, B, D)
+    out = [torch.empty_like(x) for _ in range(6)]
+    av.av_scan(x, gate, out[0])
+    av.av_scan(x, gate.contiguous(), out[1])
+    av.av_scan_backward(x, gate, out[0], dy, out[2], out[3])
+    av.av_scan_backward(x, gate.contiguous(), out[0], dy.contiguous(), out[4], out[5])
+    for a, b in ((0, 1), (2, 4), (3, 5)):
+        assert torch.equal(out[a], out[b])
+    with pytest.raises(av.AvError):
+        av.av_scan(x, gate, torch.empty((1, B, D), device="cuda").expand(T, B, D))
+
+
+def test_no_steps():
+    x = torch.empty((0, 3, 4), device="cuda")
+    h, last = torch.randn((3, 4), device="cuda"), torch.empty((3, 4), device="cuda")
+    dg = torch.ones(4, device="cuda")
+    av.av_scan(x, dg, x, h0=h, last=last)
+    assert torch.equal(h, last)
+    av.av_scan_backward(x, dg.clone(), x, x, x, dg, h0=h, dlast=h, dh0=last)
+    assert torch.equal(h, last) and (dg == 0).all()
+    av.av_scan(x, dg, x, last=last)
+    assert (last == 0).all()
+
+
+def test_returns_of_a_rollout():
+    """Batch.returns on the rewards and done flags of stepped environments."""
+    from paper_2407_04221_amd import inputs
+    wl = inputs.WORKLOADS["c1"].with_(B=130, T=60, L=25)
+    maps, rules, actions = inputs.make_all(wl, 0, "planted")
+    b = av.Batch.for_workload(wl)
+    b.load_rules(*rules)
+    b.reset(maps)
+    rewards, done = b.step_n(torch.from_numpy(actions).cuda())
+    after = torch.randn(130, device="cuda")
+    got = b.returns(rewards, done, 0.99, after)
+    assert bool(done.any()) and bool((rewards != 0).any())
+    want = ref.scan(host(rewards)[:, :, None], np.array([float(np.float32(0.99))]),
+                    host(after)[:, None], host(done), reverse=True)
+    ref.check(host(got)[:, :, None], want["y"], "returns")
+    assert torch.equal(b.returns(rewards, done, torch.tensor([0.99], device="cuda"), after), got)
+    b.close()
+
+
+def test_binding_refuses():
+    x = torch.zeros((4, 2, 6), device="cuda")
+    y = torch.empty_like(x)
+    bad = [
+        lambda: av.av_scan(x, x, torch.empty((4, 2, 5), device="cuda")),
+        lambda: av.av_scan(x, x.half(), y),
+        lambda: av.av_scan(x, x[0, 0, :5], y),
+        lambda: av.av_scan(x, x, y, h0=torch.zeros((2, 6), dtype=torch.float64, device="cuda")),
+        lambda: av.av_scan(x, x, y, h0=torch.zeros((6, 2), device="cuda").t()),
+        lambda: av.av_scan(x, x, y, cut=torch.zeros((4, 2), device="cuda")),
+        lambda: av.av_scan(x, x, y, cut=torch.zeros((2, 4), dtype=torch.uint8, device="cuda")),
+        lambda: av.av_scan(x.transpose(1, 2), x.transpose(1, 2), y.transpose(1, 2)),
+        lambda: av.av_scan(x.double(), x.double(), y.double()),
+        lambda: av.av_scan(x[0], x[0], y[0]),
+        lambda: av.av_scan(x, x.cpu(), y),
+        lambda: av.av_scan(x, x, y, form="other"),
+        lambda: av.av_scan(x[:, :0], x[:, :0], y[:, :0]),
+        lambda: av.av_scan_backward(x, x, y, x, y.cpu()),
+        lambda: av.av_scan_backward(x, x, y, None, y),
+    ]
+    for f in bad:
+        with pytest.raises((TypeError, ValueError, KeyError, av.AvError)):
+            f()
+    long = torch.zeros((5000, 1, 4), device="cuda")
+    with pytest.raises(av.AvError):
+        av.av_scan(long, long, long, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+def test_streams_graphs_and_workspaces():
+    """A side stream; two captured launches with workspaces of their own, replayed between eager
+    launches; the same call twice gives the same bits."""
+    T, B, D = 6000, 2, 10
+    x = [torch.randn((T, B, D), device="cuda") for _ in range(2)]
+    gate, dy = torch.rand(D, device="cuda"), torch.randn((T, B, D), device="cuda")
+    want = []
+    for v in x:
+        y, dx, dg = torch.empty_like(v), torch.empty_like(v), torch.empty_like(gate)
+        av.av_scan(v, gate, y)
+        av.av_scan_backward(v, gate, y, dy, dx, dg)
+        want.append((y, dx, dg))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y = torch.empty_like(x[0])
+        av.av_scan(x[0], gate, y)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(y, want[0][0])
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for v in x:
+        out = (torch.zeros_like(v), torch.zeros_like(v), torch.zeros_like(gate))
+        ws = torch.empty(av.av_scan_workspace(T, B, D, True, True), dtype=torch.uint8, device="cuda")
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            av.av_scan(v, gate, out[0], workspace=ws)
+            av.av_scan_backward(v, gate, out[0], dy, out[1], out[2], workspace=ws)
+        graphs.append((g, ws))
+        outs.append(out)
+    for _ in range(3):
+        for g, _ in graphs:
+            g.replay()
+        y2 = torch.empty_like(y)
+        av.av_scan(x[0], gate, y2)
+        torch.cuda.synchronize()
+        assert torch.equal(y2, want[0][0])
+        for out, w in zip(outs, want):
+            for a, b in zip(out, w):
+                assert torch.equal(a, b)
+                a.zero_()

@@ -1,0 +1,401 @@
+"""av_log_probs, av_log_probs_backward and av_draw_actions on the GPU against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import learn_ref as ref
+import paper_2407_04221_amd as av
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+IDS = {"u8": torch.uint8, "i32": torch.int32, "i64": torch.int64}
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def rows_of(N, A, dtype, pad=0, shift=0):
+    flat = torch.full((shift + N * (A + pad),), 9.0, dtype=TYPES[dtype], device="cuda")
+    return flat[shift:].view(N, A + pad)[:, :A]
+
+
+def compare(logits, ids, dtype, top=0, back_pad=0, back_shift=0, seed=0):
+    """Forward and gradient of these logits (device [N][A]) and ids (numpy) against 64 bits."""
+    N, A = logits.shape
+    r = np.random.default_rng(seed)
+    wide = torch.from_numpy(ids).to("cuda")
+    f = dict(dtype=torch.float32, device="cuda")
+    logp, ent, stats = torch.empty(N, **f), torch.empty(N, **f), torch.empty((N, 2), **f)
+    tl = ti = None
+    if top:
+        tl, ti = torch.empty((N, top), **f), torch.empty((N, top), dtype=torch.int32, device="cuda")
+    av.av_log_probs(logits, wide, logp, ent, stats, tl, ti)
+    g = torch.from_numpy(r.normal(size=N)).float().cuda()
+    gh = torch.from_numpy(r.normal(size=N)).float().cuda()
+    d = rows_of(N, A, dtype, back_pad, back_shift)
+    av.av_log_probs_backward(logits, wide, stats, ent, g, gh, d)
+    want = ref.tokens(host(logits), ids.astype(np.int64), host(g), host(gh), top, dtype)
+    where = f"(N {N}, A {A}, {dtype})"
+    ref.check(host(logp), want["logp"], "logp " + where)
+    ref.check(host(ent), want["entropy"], "entropy " + where)
+    if top:
+        assert np.array_equal(ti.cpu().numpy(), want["top_ids"]), "top_ids " + where
+        ref.check(host(tl), want["top_logp"], "top_logp " + where)
+    ref.check(host(d), want["dlogits"], "dlogits " + where, dtype)
+    return logp, ent, stats, d
+
+
+def some(N, A, dtype, seed=0, scale=2.0, pad=0, shift=0, masked=0.0):
+    r = np.random.default_rng(seed)
+    v = torch.from_numpy(r.normal(size=(N, A)) * scale)
+    if masked:
+        v[torch.from_numpy(r.random((N, A)) < masked)] = -np.inf
+    logits = rows_of(N, A, dtype, pad, shift)
+    logits.copy_(v)
+    return logits, r
+
+
+SIZES = [1, 2, 3, 4, 5, 8, 9, 16, 17, 63, 64, 65, 255, 511, 513, 1023, 1025, 2041, 2047, 2048, 2049,
+         5000, 16385]
+
+
+@pytest.mark.parametrize("A", SIZES)
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_sizes(A, dtype):
+    logits, r = some(7, A, dtype)
+    compare(logits, r.integers(-1, A + 1, size=7), dtype, top=min(A, 6))
+
+
+@pytest.mark.parametrize("N,A", [(1, 5), (255, 5), (256, 5), (257, 5), (1000, 3), (5, 100), (1, 70000),
+                                 (600, 2500), (511, 4100), (3000, 40)])
+def test_rows(N, A):
+    for dtype in ("f32", "bf16"):
+        logits, r = some(N, A, dtype)
+        compare(logits, r.integers(0, A, size=N), dtype, top=3)
+
+
+@pytest.mark.parametrize("ids", ["u8", "i32", "i64"])
+def test_id_types_and_padding(ids):
+    for A in (5, 300, 3001):
+        logits, r = some(50, A, "f32")
+        v = r.integers(0, min(A, 256), size=50)
+        v[::7] = 255 if ids == "u8" else -1
+        if ids == "i64":
+            v[1::7] = 1 << 32                              # not id 0
+        logp, *_ = compare(logits, v.astype({"u8": np.uint8, "i32": np.int32, "i64": np.int64}[ids]),
+                           "f32")
+        if A == 5:
+            assert (logp[::7] == 0).all()
+
+
+@pytest.mark.parametrize("pad,shift,bpad,bshift", [(0, 0, 0, 0), (1, 0, 1, 0), (3, 1, 3, 1),
+                                                   (8, 0, 0, 0), (0, 1, 0, 2), (7, 5, 1, 3)])
+@pytest.mark.parametrize("A", [5, 130, 2600])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_strides(pad, shift, bpad, bshift, A, dtype):
+    """Rows and their gradients at any distance from a word's border; what lies between is left."""
+    logits, r = some(9, A, dtype, pad=pad, shift=shift)
+    *_, d = compare(logits, r.integers(0, A, size=9), dtype, top=4, back_pad=bpad,
+                    back_shift=bshift)
+    if bpad:
+        between = d.as_strided((9, bpad), (A + bpad, 1), d.storage_offset() + A)[:-1]
+        assert (between == 9.0).all()
+
+
+@pytest.mark.parametrize("A", [5, 100, 2000, 9000])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_masks(A, dtype):
+    """Masked choices, given tokens among them, and rows that a mask leaves one or no choice."""
+    logits, r = some(12, A, dtype, masked=0.5)
+    logits[0] = -np.inf                                    # nothing left
+    logits[1] = -np.inf
+    logits[1, A - 1] = 3.0                                 # one left, the last
+    logits[2] = -np.inf
+    logits[2, 0] = -7.0
+    lowest = torch.finfo(TYPES[dtype]).min
+    logits[3] = lowest                                     # all of the lowest value: uniform
+    logits[4] = lowest
+    logits[4, A // 2] = 0.0
+    logits[5] = torch.finfo(TYPES[dtype]).max
+    logits[6, ::2] = lowest
+    ids = r.integers(0, A, size=12)
+    ids[2], ids[4] = A - 1, 0                              # masked, and all but masked
+    logp, ent, _, d = compare(logits, ids, dtype, top=min(A, 8))
+    assert logp[0] == -np.inf and ent[0] == 0 and (d[0] == 0).all()
+    assert logp[2] == -np.inf and ent[1] == 0
+
+
+@pytest.mark.parametrize("A", [3, 60, 1500, 7000])
+def test_infinities_and_nan(A):
+    """A row with a NaN or +inf is NaN throughout and leaves its neighbours alone."""
+    logits, r = some(8, A, "f32")
+    logits[1, A - 1] = float("nan")
+    logits[3, A // 2] = float("inf")
+    logits[5] = float("nan")
+    logits[6] = -np.inf
+    logits[6, A - 1] = float("nan")
+    ids = r.integers(0, A, size=8)
+    ids[5] = -1
+    logp, ent, _, d = compare(logits, ids, "f32", top=2)
+    assert logp[5] == 0 and torch.isnan(ent[5])
+
+
+@pytest.mark.parametrize("A", [16, 500, 2048, 3000, 40000])
+@pytest.mark.parametrize("order", ["equal", "rising", "falling", "steps", "one_thread"])
+def test_alternatives_of_hard_orders(A, order):
+    """Ties, and rows whose largest values sit together: the lowest index of equal ones first."""
+    i = torch.arange(A, dtype=torch.float64)
+    v = {"equal": i * 0, "rising": i / A * 4, "falling": -i / A * 4, "steps": -(i // 37 % 5),
+         "one_thread": torch.where(i % 1024 < 8, i / A, i * 0 - 1)}[order]
+    for dtype in ("f32", "bf16"):
+        for top in (1, 32 if A > 32 else A):
+            for N in (2, 600 if A == 3000 else 3):
+                logits = rows_of(N, A, dtype)
+                logits.copy_(v.expand(N, A))
+                compare(logits, np.zeros(N, np.int64), dtype, top=top)
+
+
+def test_more_alternatives_than_choices():
+    logits, _ = some(4, 3, "f32")
+    compare(logits, np.zeros(4, np.int64), "f32", top=5)
+    zero = torch.tensor([[0.0, -0.0, 0.0]], device="cuda")
+    compare(zero, np.zeros(1, np.int64), "f32", top=3)
+
+
+def test_confident_and_wide_rows():
+    for scale in (0.0, 1e-3, 30.0, 1e4):
+        for A in (5, 1000, 6000):
+            logits, r = some(6, A, "f32", scale=scale)
+            compare(logits, r.integers(0, A, size=6), "f32", top=2)
+
+
+def test_parts_on_request():
+    """Any output alone, either gradient alone, and the gradient in place."""
+    for A in (5, 300, 4000):
+        logits, r = some(10, A, "f32")
+        ids = torch.from_numpy(r.integers(0, A, size=10)).cuda()
+        f = dict(device="cuda")
+        logp, ent, stats = torch.empty(10, **f), torch.empty(10, **f), torch.empty((10, 2), **f)
+        av.av_log_probs(logits, ids, logp, ent, stats)
+        a, b, c = torch.empty(10, **f), torch.empty(10, **f), torch.empty((10, 2), **f)
+        av.av_log_probs(logits, ids, a)
+        av.av_log_probs(logits, entropy=b)
+        av.av_log_probs(logits, stats=c)
+        assert torch.equal(a, logp) and torch.equal(b, ent) and torch.equal(c, stats)
+        g, gh, zero = torch.randn(10, **f), torch.randn(10, **f), torch.zeros(10, **f)
+        d = [torch.empty_like(logits) for _ in range(5)]
+        av.av_log_probs_backward(logits, ids, stats, None, g, None, d[0])
+        av.av_log_probs_backward(logits, ids, stats, ent, g, zero, d[1])
+        av.av_log_probs_backward(logits, None, stats, ent, None, gh, d[2])
+        av.av_log_probs_backward(logits, ids, stats, ent, zero, gh, d[3])
+        assert torch.equal(d[0], d[1]) and torch.equal(d[2], d[3])
+        av.av_log_probs_backward(logits, ids, stats, ent, g, gh, d[4])
+        same = logits.clone()
+        av.av_log_probs_backward(same, ids, stats, ent, g, gh, same)
+        assert torch.equal(same, d[4])
+
+
+def test_one_row_for_all():
+    """A row stride of 0.  (The rows of a copy start at other places of a 16-byte word, so their sums
+    are taken in another order: both are held to the bound, not to each other's bits.)"""
+    row = torch.randn((1, 50), device="cuda")
+    logits, ids = row.expand(20, 50), torch.arange(20, device="cuda")
+    a, b = torch.empty(20, device="cuda"), torch.empty(20, device="cuda")
+    av.av_log_probs(logits, ids, a)
+    av.av_log_probs(logits.contiguous(), ids, b)
+    want = ref.tokens(host(logits), np.arange(20))
+    ref.check(host(a), want["logp"], "logp, one row for all")
+    ref.check(host(b), want["logp"], "logp, copied rows")
+    with pytest.raises(av.AvError):
+        av.av_log_probs_backward(logits, ids, torch.empty((20, 2), device="cuda"), None, a, None,
+                                 torch.empty((1, 50), device="cuda").expand(20, 50))
+
+
+@pytest.mark.parametrize("A", [1, 2, 5, 8, 9, 17, 64, 65, 255, 256])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_draw(A, dtype):
+    for N in (1, 131, 1000):
+        logits, r = some(N, A, dtype, masked=0.3, pad=A % 3)
+        if N > 1:
+            logits[0] = -np.inf
+            logits[1, A - 1] = float("nan")
+            logits[2, A // 2] = float("inf")
+            logits[3] = 0.0
+        u = r.random(N).astype(np.float32)
+        u[-3:] = (0.0, 1.0 - 2.0 ** -24, 1.0)[-min(3, N):]
+        actions = torch.empty(N, dtype=torch.uint8, device="cuda")
+        logp = torch.empty(N, device="cuda")
+        av.av_draw_actions(logits, torch.from_numpy(u).cuda(), actions, logp)
+        want, want_logp = ref.draw(host(logits), u)
+        assert np.array_equal(actions.cpu().numpy(), want)
+        # rounded once from 64 bits
+        ref.check(host(logp), (want_logp, ref.U * np.abs(np.nan_to_num(want_logp)) + 1e-12), "logp")
+        again = torch.empty_like(actions)
+        av.av_draw_actions(logits, torch.from_numpy(u).cuda(), again)
+        assert torch.equal(again, actions)
+
+
+def test_draw_follows_the_distribution():
+    """Numbers spread evenly over [0, 1) draw each choice as often as its probability says, to one
+    draw either side of each border."""
+    N = 4096
+    p = np.array([0.1, 0.0, 0.4, 0.25, 0.25])
+    with np.errstate(divide="ignore"):
+        logits = torch.from_numpy(np.log(p)).float().cuda().expand(N, 5)
+    u = (torch.arange(N, device="cuda") + 0.5) / N
+    actions = torch.empty(N, dtype=torch.uint8, device="cuda")
+    av.av_draw_actions(logits, u, actions)
+    count = np.bincount(actions.cpu().numpy(), minlength=5)
+    assert (np.abs(count - p * N) <= 2).all() and count[1] == 0
+
+
+def test_binding_refuses():
+    l = torch.zeros((4, 6), device="cuda")
+    ids, f = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
+    st = torch.zeros((4, 2), device="cuda")
+    top_i = torch.zeros((4, 2), dtype=torch.int32, device="cuda")
+    bad = [
+        lambda: av.av_log_probs(l.double(), ids, f),
+        lambda: av.av_log_probs(l.t(), torch.zeros(6, dtype=torch.int64, device="cuda"),
+                                torch.zeros(6, device="cuda")),
+        lambda: av.av_log_probs(l, ids.to(torch.int16), f),
+        lambda: av.av_log_probs(l, ids[:3], f),
+        lambda: av.av_log_probs(l, ids, f[:3]),
+        lambda: av.av_log_probs(l, ids),
+        lambda: av.av_log_probs(l, ids, f, top_logp=st),
+        lambda: av.av_log_probs(l, ids, f, top_logp=st, top_ids=top_i.long()),
+        lambda: av.av_log_probs(l, ids, f, top_logp=torch.zeros((4, 33), device="cuda"),
+                                top_ids=torch.zeros((4, 33), dtype=torch.int32, device="cuda")),
+        lambda: av.av_log_probs_backward(l, ids, st, None, f, f, torch.empty_like(l)),
+        lambda: av.av_log_probs_backward(l, None, st, f, f, f, torch.empty_like(l)),
+        lambda: av.av_log_probs_backward(l, ids, st, f, f, f, torch.empty_like(l).half()),
+        lambda: av.av_draw_actions(torch.zeros((4, 257), device="cuda"), f,
+                                   torch.zeros(4, dtype=torch.uint8, device="cuda")),
+        lambda: av.av_draw_actions(l, f, ids),
+        lambda: av.av_draw_actions(l, f.double(), torch.zeros(4, dtype=torch.uint8, device="cuda")),
+    ]
+    for g in bad:
+        with pytest.raises((TypeError, ValueError, av.AvError)):
+            g()
+
+
+def test_streams_and_graphs():
+    l = torch.randn((300, 5000), device="cuda")
+    ids = torch.arange(300, device="cuda")
+    f = dict(device="cuda")
+    outs = []
+    for _ in range(2):
+        outs.append([torch.zeros(300, **f), torch.zeros(300, **f), torch.zeros((300, 2), **f),
+                     torch.zeros((300, 4), **f), torch.zeros((300, 4), dtype=torch.int32, **f),
+                     torch.zeros_like(l), torch.zeros(300, dtype=torch.uint8, **f)])
+    g, u = torch.randn(300, **f), torch.rand(300, **f)
+
+    def call(o):
+        av.av_log_probs(l, ids, *o[:5])
+        av.av_log_probs_backward(l, ids, o[2], o[1], g, g, o[5])
+        av.av_draw_actions(l[:, :200], u, o[6])
+    call(outs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[1])
+    for _ in range(3):
+        graph.replay()
+        call(outs[0])
+        torch.cuda.synchronize()
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
+            b.zero_()
+
+
+def test_an_agent_learns_from_a_rollout():
+    """The operators together, as a policy gradient uses them: actions drawn for every step of a
+    batch, returns of its rewards and done flags, the agent's memory over the rollout, the
+    log-probabilities of the drawn actions, and the gradient back through all of it, against the same
+    chain in 64 bits."""
+    from paper_2407_04221_amd import inputs
+    wl = inputs.WORKLOADS["c1"].with_(B=70, L=9)
+    maps, rules, _ = inputs.make_all(wl.with_(T=2), 0, "planted")
+    b = av.Batch.for_workload(wl)
+    b.load_rules(*rules)
+    b.reset(maps)
+    T, B, D, w = 20, wl.B, 24, 5
+    r = np.random.default_rng(5)
+    obs_n = wl.C * w * w
+    W1 = torch.from_numpy(r.normal(size=(obs_n, 2 * D)) * 0.1).float().cuda()
+    W2 = torch.from_numpy(r.normal(size=(D, 5)) * 0.5).float().cuda()
+    uniform = torch.from_numpy(r.random((T, B))).float().cuda()
+    obs = b.observe(w).reshape(B, obs_n).float()
+    state = torch.zeros((B, D), device="cuda")
+    seen, acted, rewards, done, drawn_logp = [], [], [], [], []
+    was_done = torch.zeros(B, dtype=torch.uint8, device="cuda")
+    flags = []
+    y1 = torch.empty((1, B, D), device="cuda")
+    for t in range(T):                          # acting: one token of every environment at a time
+        h = obs @ W1
+        flags.append(was_done.clone())
+        av.av_scan(h[None, :, :D], h[None, :, D:], y1, h0=state, last=state, cut=was_done[None],
+                   form="gated")
+        actions, logp = b.act(state @ W2, uniform[t])
+        seen.append(obs)
+        acted.append(actions)
+        drawn_logp.append(logp)
+        rew, dn, window = b.step_observe(actions[None], w)
+        rewards.append(rew[0])
+        done.append(dn[0])
+        was_done = dn[0].clone()
+        obs = window.reshape(B, obs_n).float()
+    rewards, done, flags = torch.stack(rewards), torch.stack(done), torch.stack(flags)
+    acted, drawn_logp = torch.stack(acted), torch.stack(drawn_logp)
+    assert bool(done.any())
+    # learning: the same states from one scan over the rollout
+    ret = b.returns(rewards, done, 0.9)
+    X = torch.stack(seen)
+    h = X @ W1
+    x, gate = h[:, :, :D], h[:, :, D:]
+    y = torch.empty((T, B, D), device="cuda")
+    av.av_scan(x, gate, y, cut=flags, form="gated")
+    logits = (y.reshape(T * B, D) @ W2).contiguous()
+    n = T * B
+    logp, ent, st = (torch.empty(n, device="cuda"), torch.empty(n, device="cuda"),
+                     torch.empty((n, 2), device="cuda"))
+    av.av_log_probs(logits, acted.reshape(n), logp, ent, st)
+    dlogits = torch.empty_like(logits)
+    dlogp = (-ret / n).reshape(n)
+    dent = torch.full((n,), -0.01 / n, device="cuda")
+    av.av_log_probs_backward(logits, acted.reshape(n), st, ent, dlogp, dent, dlogits)
+    dy = (dlogits @ W2.t()).view(T, B, D)
+    dh = torch.empty_like(h)
+    av.av_scan_backward(x, gate, y, dy, dh[:, :, :D], dh[:, :, D:], cut=flags, form="gated")
+    dW1 = X.reshape(n, obs_n).t() @ dh.reshape(n, 2 * D)
+    # in 64 bits, on the host, by torch's own differentiation
+    V1, V2 = W1.double().cpu().requires_grad_(), W2.double().cpu().requires_grad_()
+    s = torch.zeros((B, D), dtype=torch.float64)
+    F, Xh, total, logps, acts = flags.cpu(), X.double().cpu(), 0.0, [], acted.cpu().long()
+    rh = torch.zeros(B, dtype=torch.float64)
+    rets = []
+    for t in reversed(range(T)):
+        rh = rewards[t].double().cpu() + 0.9 * rh * (done[t].cpu() == 0)
+        rets.append(rh)
+    rets = torch.stack(rets[::-1])
+    for t in range(T):
+        z = Xh[t] @ V1
+        s = torch.where(F[t][:, None] != 0, 0.0, s)
+        a = torch.sigmoid(z[:, D:])
+        s = a * s + (1 - a) * z[:, :D]
+        lp = torch.log_softmax(s @ V2, 1)
+        own = lp.gather(1, acts[t][:, None])[:, 0]
+        logps.append(own)
+        H = -(lp.exp() * lp).sum(1)
+        total = total - (rets[t] * own).sum() / n - 0.01 / n * H.sum()
+    total.backward()
+    logps = torch.stack(logps).detach()
+    # 32-bit products over obs_n, 2 D and n terms between the operators, each term of order one at
+    # most: n U with n the longest sum, and twenty steps of memory
+    tol = (obs_n + D + 20 * 20) * ref.U * 4
+    assert float((logp.view(T, B).double().cpu() - logps).abs().max()) < tol
+    assert float((drawn_logp.double().cpu() - logps).abs().max()) < tol
+    scale = float(V1.grad.abs().max())
+    assert float((dW1.double().cpu() - V1.grad).abs().max()) < scale * (n + obs_n) * ref.U * 4
+    b.close()
