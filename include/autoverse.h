@@ -440,7 +440,8 @@ typedef enum {
 
 /* Shape and layout of a recurrence: `rows` sequences of `steps` steps and `width` values.
  * Element (t, b, d) of a tensor is at t * its step stride + b * its row stride + d (in elements;
- * the width is contiguous).  Inputs may have strides of 0 (a broadcast input). */
+ * the width is contiguous).  Strides are not negative; inputs may have strides of 0 (a broadcast
+ * input). */
 typedef struct {
     int64_t steps;            /* T in [0, 2^31) */
     int64_t rows, width;      /* B >= 0, D >= 1, B x D < 2^31 */
@@ -500,7 +501,7 @@ typedef struct {
     int64_t choices;          /* A in [1, 2^31 - 1025] */
     int32_t dtype;            /* av_dtype of the logits and their gradient */
     int32_t ids_type;         /* av_ids_type */
-    int64_t row_stride;       /* of the logits, in elements (0: one row for all) */
+    int64_t row_stride;       /* of the logits, in elements, >= 0 (0: one row for all) */
     int64_t drow_stride;      /* of dlogits (av_log_probs_backward) */
     int32_t top;              /* alternatives per row, in [0, AV_TOP_MAX] */
     int32_t device;

@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -46,11 +48,25 @@ def check_template(verbose: bool = False) -> None:
 def build(out: str = LIB, verbose: bool = False) -> str:
     embed_template()
     check_template(verbose)
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    cmd = [HIPCC, *FLAGS, "-x", "hip", *srcs, "-lhiprtc", "-o", out + ".tmp"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True, cwd=CSRC)
+    compile_flags = [f for f in FLAGS if f != "-shared"]
+
+    def one(source: str, objects: str) -> str:
+        obj = os.path.join(objects, source + ".o")
+        cmd = [HIPCC, *compile_flags, "-x", "hip", "-c", os.path.join(CSRC, source), "-o", obj]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True, cwd=CSRC)
+        return obj
+
+    with tempfile.TemporaryDirectory(prefix="autoverse_build_") as objects, \
+            ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        # the longest to compile first
+        order = sorted(SOURCES, key=lambda f: not f.startswith("k_scan"))
+        objs = list(pool.map(lambda f: one(f, objects), order))
+        cmd = [HIPCC, *FLAGS, *objs, "-lhiprtc", "-o", out + ".tmp"]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True, cwd=CSRC)
     os.replace(out + ".tmp", out)
     return out
 

@@ -303,7 +303,6 @@ hipError_t launch_group_step(const StepArgs &a, hipStream_t s);
 // stride carries the sign of the order; the gradient is processed from the last step to the
 // first.  first / final: the state (or its gradient) before the first processed step and after
 // the last one.
-constexpr int kScanSteps = 8;         // consecutive steps a wave holds in registers
 struct ScanArgs {
     int64_t T, N, D, chunk;           // steps, columns B x D, width, steps per chunk
     const void *x, *gate, *y, *dy;
@@ -317,12 +316,13 @@ struct ScanArgs {
         dgate_step, dgate_row, cut_step, cut_row;
 };
 struct ScanPlan {
-    int vec, waves, chunks, runs;     // columns a lane, waves a workgroup, chunks of time, and
-                                      // runs of rows in the first sum of a gate per value
+    int vec, waves, chunks, runs;     // columns a lane; waves a workgroup (0: a lane takes its
+                                      // columns through all steps); chunks of time; runs of rows
+                                      // in the first sum of a gate per value
     int64_t chunk;                    // steps
     size_t part_off, bytes;           // workspace: slots, then the sums
 };
-ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, bool pairs, bool col, bool back);
+ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int wide, bool far, bool col, bool back);
 hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool gated, bool col,
                        bool back, hipStream_t s);
 

@@ -75,7 +75,7 @@ av_status check_scan(const av_scan_config *c) {
 // The elements of an output must not share a place: of two dimensions the one with the longer
 // stride steps over all of the other.
 bool spread(int64_t step, int64_t row, const av_scan_config &c) {
-    std::pair<int64_t, int64_t> dim[2] = {{std::llabs(step), c.steps}, {std::llabs(row), c.rows}};
+    std::pair<int64_t, int64_t> dim[2] = {{step, c.steps}, {row, c.rows}};
     if (dim[1].first < dim[0].first) std::swap(dim[0], dim[1]);
     int64_t extent = c.width;
     for (const auto &d : dim) {
@@ -91,23 +91,22 @@ struct Place {
     int64_t step, row;
 };
 
-// Offsets in bytes stay far inside 64 bits.
+// Offsets are not negative and stay far inside 64 bits.
 bool reachable(int64_t step, int64_t n) {
-    const __int128 far = __int128(step) * n;
-    return far < (__int128(1) << 60) && far > -(__int128(1) << 60);
+    return step >= 0 && __int128(step) * n < (__int128(1) << 60);
 }
 
-bool whole_pairs(const Place &a, size_t size) {
-    return reinterpret_cast<uintptr_t>(a.p) % (2 * size) == 0 && a.step % 2 == 0 && a.row % 2 == 0;
+// Whether groups of n neighbouring values are aligned words throughout.
+bool whole(const Place &a, size_t size, int n) {
+    return reinterpret_cast<uintptr_t>(a.p) % (n * size) == 0 && a.step % n == 0 && a.row % n == 0;
 }
 
 size_t workspace_of(const av_scan_config &c, bool back) {
     size_t most = 0;
-    for (int pairs = 0; pairs < 2; ++pairs) {
-        if (pairs && c.width % 2) continue;
-        most = std::max(most, scan_plan(c.steps, c.rows, c.width, pairs != 0, c.gate_per_value != 0,
-                                        back).bytes);
-    }
+    for (int wide : {1, int(8 / size_of(c.dtype))})
+        if (c.width % wide == 0)
+            most = std::max(most, scan_plan(c.steps, c.rows, c.width, wide, false,
+                                            c.gate_per_value != 0, back).bytes);
     return most;
 }
 
@@ -141,14 +140,23 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     for (const float *p : floats)
         if (reinterpret_cast<uintptr_t>(p) % 4) return bad("a state is not aligned to its type");
 
-    bool pairs = c.width % 2 == 0 && whole_pairs(po, size);
-    if (reads_x) pairs = pairs && whole_pairs(px, size);
-    if (col) pairs = pairs && reinterpret_cast<uintptr_t>(gate) % (2 * size) == 0;
-    else pairs = pairs && whole_pairs(pg, size);
-    if (back) pairs = pairs && whole_pairs(py, size) && whole_pairs(pdy, size);
-    if (back && dgate && !col) pairs = pairs && whole_pairs(pdg, size);
+    int wide = int(8 / size);
+    bool words = c.width % wide == 0 && whole(po, size, wide);
+    if (reads_x) words = words && whole(px, size, wide);
+    if (col) words = words && reinterpret_cast<uintptr_t>(gate) % 8 == 0;
+    else words = words && whole(pg, size, wide);
+    if (back) words = words && whole(py, size, wide) && whole(pdy, size, wide);
+    if (back && dgate && !col) words = words && whole(pdg, size, wide);
+    for (const float *p : floats) words = words && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+    if (!words) wide = 1;
 
-    ScanPlan plan = scan_plan(c.steps, c.rows, c.width, pairs, col, back);
+    // a wave reaches the rows of its columns by 32-bit distances
+    const int64_t span = std::min(c.rows, 64 * wide / c.width + 2);
+    bool far = false;
+    for (const Place &a : everything)
+        if (a.p) far = far || span * a.row + c.width >= (int64_t(1) << 32) / int64_t(size);
+
+    ScanPlan plan = scan_plan(c.steps, c.rows, c.width, wide, far, col, back);
     if (some && workspace_of(c, back) > 0) {
         if (!workspace || workspace_bytes < workspace_of(c, back))
             return bad("workspace of %zu bytes; %zu are needed", workspace ? workspace_bytes : 0,
@@ -287,7 +295,7 @@ av_status av_log_probs_backward(const av_tokens_config *cfg, const void *logits,
     if (dlogp && !ids) return bad("dlogp needs ids");
     if (dentropy && !entropy) return bad("dentropy needs entropy");
     if (!reachable(cfg->drow_stride, cfg->rows)) return bad("drow_stride is out of range");
-    if (cfg->rows > 1 && std::llabs(cfg->drow_stride) < cfg->choices)
+    if (cfg->rows > 1 && cfg->drow_stride < cfg->choices)
         return bad("drow_stride %lld: the rows of dlogits overlap", (long long)cfg->drow_stride);
     if (!aligned(logits, size_of(cfg->dtype)) || !aligned(dlogits, size_of(cfg->dtype)) ||
         !aligned(ids, ids_size(cfg->ids_type)) || !aligned(stats, 8) || !aligned(entropy, 4) ||

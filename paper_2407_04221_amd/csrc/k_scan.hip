@@ -28,7 +28,12 @@
 namespace av {
 namespace {
 
-constexpr int kWaves = 8;       // most waves of a workgroup
+// Steps a wave holds, and most waves of a workgroup: a lane with one column holds 8 steps, one with
+// a word of columns 4, which leaves registers for more waves a SIMD (4 columns x 8 steps of the
+// gradient need 183 registers and run at two waves a SIMD).
+constexpr int steps_of(int V) { return V == 1 ? 8 : 4; }
+constexpr int waves_of(int V) { return V == 1 ? 16 : 8; }
+template <typename T> constexpr int kWide = 8 / sizeof(T);      // columns of a lane's 8-byte word
 constexpr int kFill = 512;      // workgroups that fill the device's 256 compute units
 
 // 1 / (1 + e^-g) and its complement, each to full relative precision.
@@ -43,151 +48,260 @@ __device__ inline float follow(float2 span, float s) {
     return span.x != span.x ? span.y : fmaf(span.x, s, span.y);
 }
 
-// What a lane keeps of its place: the column, and where its elements start.
-template <int V> struct Column {
-    int n;                      // first column, n = b * D + d
+// V states of neighbouring columns, moved as words of up to 16 bytes.
+template <int V> struct alignas(V >= 4 ? 16 : 4) States { float v[V]; };
+
+template <int V> __device__ inline States<V> states_at(const float *p, int64_t n) {
+    States<V> s;
+    if (p) {
+        s = *reinterpret_cast<const States<V> *>(p + n);
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) s.v[v] = 0.0f;
+    }
+    return s;
+}
+
+// A lane's place: its first column n = b D + d, and whether it has one (a lane past the end
+// repeats the last columns and stores nothing).
+struct Column {
+    int n;
     bool live;
-    int64_t b, d;
+    uint32_t b, d;
 };
 
-template <int V> __device__ inline Column<V> column_of(const ScanArgs &p, int lane) {
-    Column<V> c;
-    const int64_t n = (int64_t(blockIdx.x) * 64 + lane) * V;
-    c.live = n < p.N;
-    c.n = int(c.live ? n : p.N - V);          // a lane past the end repeats the last columns
+template <int V> __device__ inline Column column_of(const ScanArgs &p, int64_t place) {
+    Column c;
+    c.live = place * V < p.N;
+    c.n = int(c.live ? place * V : p.N - V);
     c.b = uint32_t(c.n) / uint32_t(p.D);
-    c.d = c.n - c.b * p.D;
+    c.d = uint32_t(c.n) - c.b * uint32_t(p.D);
     return c;
 }
 
-// K steps of one wave as they come from memory.
-template <typename T, int V, int K, bool kX, bool kGate> struct Steps {
-    Vec<T, V> x[kX ? K : 1], g[kGate ? K : 1], e[K];
+// The workgroup's group of columns.  Workgroups are dealt to the 8 XCDs in turn; here each XCD takes
+// one contiguous eighth of the groups.  Neighbouring groups then meet in one XCD's cache, whose
+// channels lie 256 bytes apart: dealt in turn, a wave's 256-byte rows, a power of two of bytes from
+// step to step, would all fall into two of that cache's sixteen channels.
+__device__ inline int64_t group_of_columns() {
+    const uint32_t eighth = gridDim.x / 8, x = blockIdx.x;
+    return gridDim.x % 8 ? x : x % 8 * eighth + x / 8;
+}
+
+template <int kBytes> struct Bits;
+template <> struct Bits<2> { typedef uint16_t type; };
+template <> struct Bits<4> { typedef uint32_t type; };
+template <> struct Bits<8> { typedef uint64_t type; };
+
+// A tensor as one workgroup sees it: a base and a step stride in bytes that are the same for the
+// whole wave, and the lane's own distance, which the host has made sure fits 32 bits; an access
+// is then one scalar address and one 32-bit register.
+struct Lanes {
+    const char *base;
+    int64_t step;
+    uint32_t off;
+
+    __device__ Lanes(const void *p, int64_t step_, int64_t row, int size, uint32_t b0,
+                     const Column &c, bool rows = true)
+        : base(static_cast<const char *>(p) + (rows ? b0 * row : 0) * size), step(step_ * size),
+          off(((rows ? (c.b - b0) * uint32_t(row) : 0u) + c.d) * uint32_t(size)) {}
+    // A place that moves along the steps; get and put access the lane's element there.
+    struct Cursor {
+        const char *p;
+        int64_t step;
+        uint32_t off;
+        template <typename E> __device__ E get() const { return *reinterpret_cast<const E *>(p + off); }
+        // Written past the caches: outputs are not read again by the kernel, and the inputs that
+        // other workgroups still want stay.
+        template <typename E> __device__ void put(const E &e) const {
+            typedef typename Bits<sizeof(E)>::type U;
+            U u;
+            __builtin_memcpy(&u, &e, sizeof u);
+            __builtin_nontemporal_store(u, reinterpret_cast<U *>(const_cast<char *>(p) + off));
+        }
+        __device__ void next() { p += step; }
+    };
+    __device__ Cursor at(int q) const { return Cursor{base + q * step, step, off}; }
+};
+
+// K consecutive steps of V columns as they come from memory.
+template <typename T, int V, int K, bool kX, bool kGate, bool kBack> struct Raw {
+    Vec<T, V> e[K], g[kGate ? K : 1], x[kX ? K : 1], before[kBack ? K : 1];
     uint8_t cut[K];
 };
 
-// The kernels' view of one direction.  kBack: e is dy, and x is read only where gated; else e
-// holds x itself.
-template <typename T, int V, int K, bool kGated, bool kCol, bool kBack>
-struct Reader {
-    static constexpr bool kX = kBack && kGated;
-    using Raw = Steps<T, V, K, kX, !kCol>;
-    const ScanArgs &p;
-    const T *x, *g, *e;
-    const uint8_t *cut;
-    int64_t xs, gs, es;
+// The same in 32 bits: a step takes the state s to a s + b (to b where it is cut), with
+// b = x or (1 - a) x, or, in the gradient, c to a (c + e) (to 0), e the gradient of the output.
+template <int V, int K, bool kRest> struct Work {
+    float a[K][V], b[K][V], rest[kRest ? K : 1][V];
+    uint8_t cut[K];
+};
+
+// One direction's view of the tensors.  kBack: e is dy, `before` the state before the step, and x is
+// read only where gated; else e is x.
+template <typename T, int V, int K, bool kGated, bool kCol, bool kBack> struct Reader {
+    static constexpr bool kX = kBack && kGated, kRest = kBack && kGated;
+    using In = Raw<T, V, K, kX, !kCol, kBack>;
+    using Out = Work<V, K, kRest>;
+    using Values = Vec<T, V>;
+    Lanes x, g, e, y, cut;
+    int steps;
+    bool cuts;
     float ca[V], cr[V];                       // a gate per value: a and 1 - a
 
-    __device__ Reader(const ScanArgs &p, const Column<V> &c) : p(p) {
-        x = static_cast<const T *>(p.x) + c.b * p.x_row + c.d;
-        xs = p.x_step;
-        e = kBack ? static_cast<const T *>(p.dy) + c.b * p.dy_row + c.d : x;
-        es = kBack ? p.dy_step : xs;
-        g = static_cast<const T *>(p.gate) + (kCol ? c.d : c.b * p.gate_row + c.d);
-        gs = p.gate_step;
-        cut = p.cut ? p.cut + c.b * p.cut_row : nullptr;
+    __device__ Reader(const ScanArgs &p, const Column &c, uint32_t b0)
+        : x(p.x, p.x_step, p.x_row, sizeof(T), b0, c), g(p.gate, p.gate_step, p.gate_row, sizeof(T), b0, c, !kCol),
+          e(kBack ? p.dy : p.x, kBack ? p.dy_step : p.x_step, kBack ? p.dy_row : p.x_row, sizeof(T), b0, c),
+          y(p.y, p.y_step, p.y_row, sizeof(T), b0, c),
+          cut(p.cut, p.cut_step, p.cut_row, 1, b0, Column{c.n, c.live, c.b, 0}), steps(int(p.T)),
+          cuts(p.cut != nullptr) {
         if (kCol) {
+            const Values v = g.at(0).template get<Values>();
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                ca[v] = to_f32(g[v]);
-                cr[v] = 1.0f;
-                if (kGated) gate_pair(ca[v], ca[v], cr[v]);
+            for (int i = 0; i < V; ++i) {
+                ca[i] = to_f32(v.v[i]);
+                cr[i] = 1.0f;
+                if (kGated) gate_pair(ca[i], ca[i], cr[i]);
             }
         }
     }
 
-    // Steps q .. q + K - 1; past `end` the last step is read again.
-    __device__ void load(Raw &r, int64_t q, int64_t end) const {
+    // Steps q .. q + K - 1; past `end` the last step is read again.  kSpan: only what a span needs.
+    template <bool kSpan> __device__ void load(In &r, int q, int end) const {
+        q = min(q, end - 1);
+        // the state before processed step q of the gradient is the output one step on
+        Lanes::Cursor pe = e.at(q), pg = g.at(q), px = x.at(q), pc = cut.at(q),
+                      py = y.at(min(q + 1, steps - 1));
+        const bool whole = q + K < end;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int64_t t = min(q + k, end - 1);
-            if (kX) r.x[k] = *reinterpret_cast<const Vec<T, V> *>(x + t * xs);
-            if (!kCol) r.g[k] = *reinterpret_cast<const Vec<T, V> *>(g + t * gs);
-            r.e[k] = *reinterpret_cast<const Vec<T, V> *>(e + t * es);
+            r.e[k] = pe.template get<Values>();
+            if (!kCol) r.g[k] = pg.template get<Values>();
+            if (kX && !kSpan) r.x[k] = px.template get<Values>();
+            if (kBack && !kSpan) r.before[k] = py.template get<Values>();
+            if (whole || q + k + 1 < end) {
+                pe.next();
+                if (!kCol) pg.next();
+                if (kX) px.next();
+            }
+            if (kBack && (whole || q + k + 2 < steps)) py.next();
         }
-        if (cut) {
+        if (cuts) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) r.cut[k] = cut[min(q + k, end - 1) * p.cut_step];
+            for (int k = 0; k < K; ++k) {
+                r.cut[k] = pc.template get<uint8_t>();
+                if (whole || q + k + 1 < end) pc.next();
+            }
         } else {
 #pragma unroll
             for (int k = 0; k < K; ++k) r.cut[k] = 0;
         }
     }
 
-    __device__ void gate(const Raw &r, int k, int v, float &a, float &rest) const {
-        if (kCol) {
-            a = ca[v];
-            rest = cr[v];
-        } else {
-            a = to_f32(r.g[k].v[v]);
-            rest = 1.0f;
-            if (kGated) gate_pair(a, a, rest);
+    // The first n steps in r in 32 bits; the others become steps that change nothing.
+    __device__ void unpack(const In &r, int n, Out &o) const {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            o.cut[k] = r.cut[k];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float a = ca[v], rest = cr[v];
+                if (!kCol) {
+                    a = to_f32(r.g[k].v[v]);
+                    rest = 1.0f;
+                    if (kGated) gate_pair(a, a, rest);
+                }
+                const float in = to_f32(r.e[k].v[v]);
+                o.a[k][v] = a;
+                o.b[k][v] = !kBack && kGated ? rest * in : in;
+                if (kRest) o.rest[k][v] = rest;
+            }
+        }
+        if (n < K) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (k < n) continue;
+                o.cut[k] = 0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    o.a[k][v] = 1.0f;
+                    o.b[k][v] = 0.0f;
+                }
+            }
         }
     }
 
-    // The span of the n (<= K) steps held in r.
-    __device__ void span(const Raw &r, int n, float2 (&s)[V]) const {
+    static __device__ void span(const Out &o, float2 (&s)[V]) {
 #pragma unroll
         for (int v = 0; v < V; ++v) s[v] = make_float2(1.0f, 0.0f);
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (k >= n) break;
+        for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                float a, rest;
-                gate(r, k, v, a, rest);
-                const float in = to_f32(r.e[k].v[v]);
-                if (kBack) {
-                    s[v].y = r.cut[k] ? 0.0f : a * (s[v].y + in);
-                } else {
-                    const float b = kGated ? rest * in : in;
-                    s[v].y = r.cut[k] ? b : fmaf(a, s[v].y, b);
-                }
-                s[v].x = r.cut[k] ? __builtin_nanf("") : s[v].x * a;
+                if (kBack) s[v].y = o.cut[k] ? 0.0f : o.a[k][v] * (s[v].y + o.b[k][v]);
+                else s[v].y = o.cut[k] ? o.b[k][v] : fmaf(o.a[k][v], s[v].y, o.b[k][v]);
+                s[v].x = o.cut[k] ? __builtin_nanf("") : s[v].x * o.a[k][v];
+            }
+    }
+
+    // Takes V states through step k: the output, and the gradient of the gate.  first: this is the
+    // recurrence's first step (the gradient's last), whose state before is h.
+    static __device__ void step(const In &r, const Out &o, int k, bool first, const States<V> &h,
+                                float (&state)[V], float (&out)[V], float (&dgate)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float a = o.a[k][v];
+            if (kBack) {
+                const float lam = o.b[k][v] + state[v];
+                state[v] = o.cut[k] ? 0.0f : a * lam;
+                float s = first ? h.v[v] : to_f32(r.before[k].v[v]);
+                s = o.cut[k] ? 0.0f : s;
+                out[v] = kGated ? lam * o.rest[k][v] : lam;
+                // lam (s - x) a (1 - a), or lam s
+                dgate[v] = kGated ? out[v] * a * (s - to_f32(r.x[k].v[v])) : lam * s;
+            } else {
+                state[v] = o.cut[k] ? o.b[k][v] : fmaf(a, state[v], o.b[k][v]);
+                out[v] = state[v];
             }
         }
     }
 };
 
-// Composes the spans of the waves in LDS: `state` becomes the state after all of them, `mine`
-// the one that wave w starts from.
-template <int V>
-__device__ inline void compose(const float2 *spans, int W, int w, int lane, float (&state)[V],
-                               float (&mine)[V]) {
-    for (int j = 0; j < W; ++j) {
+template <typename T, int V> __device__ inline Vec<T, V> rounded(const float (&f)[V]) {
+    Vec<T, V> o;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (j == w) mine[v] = state[v];
-            state[v] = follow(spans[(j * 64 + lane) * V + v], state[v]);
-        }
-    }
+    for (int v = 0; v < V; ++v) o.v[v] = from_f32<T>(f[v]);
+    return o;
 }
 
 // First kernel of a recurrence cut into chunks: slot 0 of the workspace takes the state coming in
 // (as a span that gives it), slot s + 1 the span of chunk s.
-template <typename T, int V, int K, bool kGated, bool kCol, bool kBack>
-__global__ void __launch_bounds__(64 * kWaves) scan_chunks_kernel(ScanArgs p) {
-    __shared__ float2 spans[kWaves * 64 * V];
+template <typename T, int V, bool kGated, bool kCol, bool kBack>
+__global__ void __launch_bounds__(64 * waves_of(V)) scan_chunks_kernel(ScanArgs p) {
+    constexpr int K = steps_of(V);
+    __shared__ float2 spans[waves_of(V) * 64 * V];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int W = blockDim.x >> 6;
-    const Column<V> c = column_of<V>(p, lane);
-    const Reader<T, V, K, kGated, kCol, kBack> in(p, c);
-    const int64_t begin = int64_t(blockIdx.y) * p.chunk, part = p.chunk / W;
+    const Column c = column_of<V>(p, group_of_columns() * 64 + lane);
+    using R = Reader<T, V, K, kGated, kCol, kBack>;
+    const R in(p, c, __builtin_amdgcn_readfirstlane(c.b));
+    const int begin = int(blockIdx.y) * int(p.chunk), part = int(p.chunk) / W;
     float2 total[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) total[v] = make_float2(1.0f, 0.0f);
     // the chunk is whole (the last one has no part here) and so is each wave's share of it
-    const int64_t from = begin + w * part, to = from + part;
-    for (int64_t q = from; q < to; q += K) {
-        typename Reader<T, V, K, kGated, kCol, kBack>::Raw raw;
-        in.load(raw, q, to);
+    const int from = begin + w * part, to = from + part;
+    typename R::In raw;
+    in.template load<true>(raw, from, to);
+    for (int q = from; q < to; q += K) {
+        typename R::Out work;
+        in.unpack(raw, K, work);
+        if (q + K < to) in.template load<true>(raw, q + K, to);
         float2 s[V];
-        in.span(raw, K, s);
+        R::span(work, s);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float y = follow(s[v], total[v].y);
-            total[v] = make_float2(s[v].x * total[v].x, y);
-        }
+        for (int v = 0; v < V; ++v)
+            total[v] = make_float2(s[v].x * total[v].x, follow(s[v], total[v].y));
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) spans[(w * 64 + lane) * V + v] = total[v];
@@ -207,19 +321,30 @@ __global__ void __launch_bounds__(64 * kWaves) scan_chunks_kernel(ScanArgs p) {
     }
 }
 
-template <typename T, int V, int K, bool kGated, bool kCol, bool kBack>
-__global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs p) {
-    __shared__ float2 spans[2][kWaves * 64 * V];
+template <typename T, int V, bool kGated, bool kCol, bool kBack>
+__global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
+    constexpr int K = steps_of(V), kMost = waves_of(V);
+    // Loading a tile ahead pays where few workgroups share a compute unit; with many it only
+    // costs registers, in the gradient too many (128 x 1024 x 256 in bf16: 85 us, without 81).
+    constexpr bool kAhead = V == 1 || !kBack;
+    __shared__ float2 spans[2][kMost * 64 * V];
+    __shared__ float carry[2][64 * V];        // the state after a tile, for the next one
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int W = blockDim.x >> 6;
-    const Column<V> c = column_of<V>(p, lane);
-    Reader<T, V, K, kGated, kCol, kBack> in(p, c);
-    const int64_t begin = int64_t(blockIdx.y) * p.chunk;
-    const int64_t end = min(p.T, begin + p.chunk);
-    float state[V], mine[V];
+    const Column c = column_of<V>(p, group_of_columns() * 64 + lane);
+    using R = Reader<T, V, K, kGated, kCol, kBack>;
+    const uint32_t b0 = __builtin_amdgcn_readfirstlane(c.b);
+    const R in(p, c, b0);
+    // fewer than 2^31 steps: kMost K more do not pass 32 bits unsigned
+    const int begin = int(blockIdx.y * uint32_t(p.chunk));
+    const int end = int(min(p.T, begin + p.chunk)), tile = W * K;
+    typename R::In next;
+    if (kAhead) in.template load<false>(next, begin + w * K, end);
+    const States<V> h = states_at<V>(kBack ? p.h0 : nullptr, c.n);
+    float state[V];
     int par = 0;
     if (p.slots) {
-        // the chunks before this one: each wave composes its share of them
+        // the chunks before this one: each wave composes its share of them, all waves the shares
         const float2 *slots = static_cast<const float2 *>(p.slots);
         const int have = int(blockIdx.y) + 1, share = (have + W - 1) / W;
         float2 s[V];
@@ -228,91 +353,77 @@ __global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs p) {
         for (int j = w * share; j < min(have, (w + 1) * share); ++j) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float2 next = slots[int64_t(j) * p.N + c.n + v];
-                s[v] = make_float2(next.x * s[v].x, follow(next, s[v].y));
+                const float2 one = slots[int64_t(j) * p.N + c.n + v];
+                s[v] = make_float2(one.x * s[v].x, follow(one, s[v].y));
             }
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            spans[par][(w * 64 + lane) * V + v] = s[v];
-            state[v] = 0.0f;
-        }
+        for (int v = 0; v < V; ++v) spans[1][(w * 64 + lane) * V + v] = s[v];
         __syncthreads();
-        compose<V>(spans[par], W, w, lane, state, mine);
-        par ^= 1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) state[v] = 0.0f;
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) state[v] = follow(spans[1][(j * 64 + lane) * V + v], state[v]);
     } else {
+        const States<V> first = states_at<V>(p.first, c.n);
 #pragma unroll
-        for (int v = 0; v < V; ++v) state[v] = p.first ? p.first[c.n + v] : 0.0f;
+        for (int v = 0; v < V; ++v) state[v] = first.v[v];
     }
+    const Lanes out(p.out, p.out_step, p.out_row, sizeof(T), b0, c);
+    const Lanes dgate(p.dgate, p.dgate_step, p.dgate_row, sizeof(T), b0, c);
+    const bool with_gate = kBack && !kCol && p.dgate;
     float sum[V] = {};                        // gradient of a gate per value
-    for (int64_t tile = begin; tile < end; tile += int64_t(W) * K) {
-        const int64_t q = tile + w * K;
-        const int n = int(max(int64_t(0), min(int64_t(K), end - q)));   // this wave's steps
-        typename Reader<T, V, K, kGated, kCol, kBack>::Raw raw;
-        in.load(raw, min(q, end - 1), end);
-        Vec<T, V> before[kBack ? K : 1];
-        if (kBack) {
-            // the state before processed step q of the gradient is the output one step on
-            const T *y = static_cast<const T *>(p.y) + c.b * p.y_row + c.d;
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-                before[k] = *reinterpret_cast<const Vec<T, V> *>(
-                    y + min(q + k + 1, p.T - 1) * p.y_step);
-        }
+    for (int at = begin; at < end; at += tile) {
+        const int q = at + w * K;
+        const int n = max(0, min(K, end - q));                          // this wave's steps
+        if (!kAhead) in.template load<false>(next, q, end);
+        const typename R::In raw = next;
+        typename R::Out work;
+        in.unpack(raw, n, work);
+        // the next tile is on its way while this one is worked on
+        if (kAhead && at + tile < end) in.template load<false>(next, q + tile, end);
         if (W > 1) {
             float2 s[V];
-            in.span(raw, n, s);
+            R::span(work, s);
 #pragma unroll
             for (int v = 0; v < V; ++v) spans[par][(w * 64 + lane) * V + v] = s[v];
             __syncthreads();
-            compose<V>(spans[par], W, w, lane, state, mine);
-            par ^= 1;
-        } else {
+            // from the state before the tile through the waves before this one
+            if (at > begin) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) mine[v] = state[v];
+                for (int v = 0; v < V; ++v) state[v] = carry[par][lane * V + v];
+            }
+#pragma unroll 4
+            for (int j = 0; j < w; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    state[v] = follow(spans[par][(j * 64 + lane) * V + v], state[v]);
+            par ^= 1;
         }
+        Lanes::Cursor po = out.at(q), pg = dgate.at(q);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (k >= n) break;
-            Vec<T, V> out, dg;
+            float o[V], dg[V];
+            R::step(raw, work, k, q + k == in.steps - 1, h, state, o, dg);
+            if (k < n) {                      // the others change nothing and are no one's output
+                if (c.live) po.put(rounded<T, V>(o));
+                if (with_gate && c.live) pg.put(rounded<T, V>(dg));
+                if (kBack && kCol) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float a, rest;
-                in.gate(raw, k, v, a, rest);
-                const float e = to_f32(raw.e[k].v[v]);
-                if (kBack) {
-                    const float lam = e + mine[v];
-                    mine[v] = raw.cut[k] ? 0.0f : a * lam;
-                    float h = to_f32(before[k].v[v]);
-                    if (q + k == p.T - 1) h = p.h0 ? p.h0[c.n + v] : 0.0f;
-                    if (raw.cut[k]) h = 0.0f;
-                    float d = lam * h;
-                    if (kGated) d = lam * (h - to_f32(raw.x[k].v[v])) * (a * rest);
-                    out.v[v] = from_f32<T>(kGated ? lam * rest : lam);
-                    if (kCol) sum[v] += d;
-                    else dg.v[v] = from_f32<T>(d);
-                } else {
-                    const float b = kGated ? rest * e : e;
-                    mine[v] = raw.cut[k] ? b : fmaf(a, mine[v], b);
-                    out.v[v] = from_f32<T>(mine[v]);
+                    for (int v = 0; v < V; ++v) sum[v] += dg[v];
                 }
             }
-            if (c.live) {
-                T *to = static_cast<T *>(p.out) + c.b * p.out_row + c.d + (q + k) * p.out_step;
-                *reinterpret_cast<Vec<T, V> *>(to) = out;
-                if (kBack && !kCol && p.dgate) {
-                    T *at = static_cast<T *>(p.dgate) + c.b * p.dgate_row + c.d +
-                            (q + k) * p.dgate_step;
-                    *reinterpret_cast<Vec<T, V> *>(at) = dg;
-                }
-            }
+            po.next();
+            pg.next();
         }
-        if (W == 1) {
+        if (W > 1 && w == W - 1) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) state[v] = mine[v];
+            for (int v = 0; v < V; ++v) carry[par][lane * V + v] = state[v];
         }
     }
-    if (p.final && w == 0 && c.live && end == p.T) {
+    // the last wave went through every step (those past the end change nothing)
+    if (p.final && w == W - 1 && c.live && end == in.steps) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p.final[c.n + v] = state[v];
     }
@@ -333,18 +444,52 @@ __global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs p) {
     }
 }
 
-// Sums m rows of `width` floats into one row (to_type T): a workgroup takes up to 64 values, its
+// A few steps (an agent's acting step is one): a lane takes its columns through all of them.  Its
+// addresses are 64 bits a lane, so any distance between rows will do.
+template <typename T, int V, bool kGated, bool kCol, bool kBack>
+__global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs p) {
+    const Column c = column_of<V>(p, int64_t(blockIdx.x) * 256 + threadIdx.x);
+    if (!c.live) return;
+    using R = Reader<T, V, 1, kGated, kCol, kBack>;
+    const R in(p, c, c.b);
+    const States<V> h = states_at<V>(kBack ? p.h0 : nullptr, c.n);
+    States<V> state = states_at<V>(p.first, c.n);
+    const Lanes out(p.out, p.out_step, p.out_row, sizeof(T), c.b, c);
+    const Lanes dgate(p.dgate, p.dgate_step, p.dgate_row, sizeof(T), c.b, c);
+    float sum[V] = {};
+    for (int q = 0; q < in.steps; ++q) {
+        typename R::In raw;
+        typename R::Out work;
+        in.template load<false>(raw, q, p.T);
+        in.unpack(raw, 1, work);
+        float o[V], dg[V];
+        R::step(raw, work, 0, q == in.steps - 1, h, state.v, o, dg);
+        out.at(q).put(rounded<T, V>(o));
+        if (kBack && !kCol && p.dgate) dgate.at(q).put(rounded<T, V>(dg));
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[v] += kBack && kCol ? dg[v] : 0.0f;
+    }
+    if (p.final) *reinterpret_cast<States<V> *>(p.final + c.n) = state;
+    if (kBack && kCol && p.part) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) p.part[c.n + v] = sum[v];
+    }
+}
+
+// Sums m rows of `width` floats into one row (to type T): a workgroup takes `lanes` values, its
 // threads share the rows, blockIdx.y takes a run of `run` rows.
 template <typename T>
-__global__ void __launch_bounds__(256) sum_rows_kernel(const float *src, int64_t m, int64_t run,
-                                                       int width, int lanes, T *dst) {
-    __shared__ float red[256];
+__global__ void __launch_bounds__(1024) sum_rows_kernel(const float *src, int64_t m, int64_t run,
+                                                        int width, int lanes, T *dst) {
+    __shared__ float red[1024];
     const int d = int(blockIdx.x) * lanes + int(threadIdx.x) % lanes;
-    const int part = int(threadIdx.x) / lanes, parts = 256 / lanes;
+    const int part = int(threadIdx.x) / lanes, parts = 1024 / lanes;
     const int64_t r0 = int64_t(blockIdx.y) * run, r1 = min(m, r0 + run);
     float s = 0.0f;
-    if (d < width)
+    if (d < width) {
+#pragma unroll 4
         for (int64_t r = r0 + part; r < r1; r += parts) s += src[r * width + d];
+    }
     red[threadIdx.x] = s;
     __syncthreads();
     for (int half = parts / 2; half > 0; half >>= 1) {
@@ -365,13 +510,25 @@ __global__ void __launch_bounds__(256) zero_kernel(T *dst, int n) {
     if (i < n) dst[i] = from_f32<T>(0.0f);
 }
 
-template <typename T, int V, int K, bool kGated, bool kCol, bool kBack>
+// Workgroups over the columns; from 64 on a multiple of 8 (group_of_columns), the last ones empty.
+unsigned scan_groups(int64_t N, int V) {
+    const int64_t n = (N / V + 63) / 64;
+    return unsigned(n < 64 ? n : (n + 7) / 8 * 8);
+}
+
+template <typename T, int V, bool kGated, bool kCol, bool kBack>
 hipError_t launch(const ScanArgs &a, const ScanPlan &plan, hipStream_t s) {
-    const unsigned tiles = unsigned((a.N / V + 63) / 64);
+    if (plan.waves == 0) {
+        const unsigned blocks = unsigned((a.N / V + 255) / 256);
+        hipLaunchKernelGGL((scan_short_kernel<T, V, kGated, kCol, kBack>), dim3(blocks), dim3(256),
+                           0, s, a);
+        return hipGetLastError();
+    }
+    const unsigned groups = scan_groups(a.N, V);
     if (plan.chunks > 1)
-        hipLaunchKernelGGL((scan_chunks_kernel<T, V, K, kGated, kCol, kBack>),
-                           dim3(tiles, plan.chunks - 1), dim3(64 * plan.waves), 0, s, a);
-    hipLaunchKernelGGL((scan_kernel<T, V, K, kGated, kCol, kBack>), dim3(tiles, plan.chunks),
+        hipLaunchKernelGGL((scan_chunks_kernel<T, V, kGated, kCol, kBack>),
+                           dim3(groups, plan.chunks - 1), dim3(64 * plan.waves), 0, s, a);
+    hipLaunchKernelGGL((scan_kernel<T, V, kGated, kCol, kBack>), dim3(groups, plan.chunks),
                        dim3(64 * plan.waves), 0, s, a);
     return hipGetLastError();
 }
@@ -379,38 +536,41 @@ hipError_t launch(const ScanArgs &a, const ScanPlan &plan, hipStream_t s) {
 template <typename T, int V, bool kGated>
 hipError_t pick(const ScanArgs &a, const ScanPlan &plan, bool col, bool back, hipStream_t s) {
     if (back)
-        return col ? launch<T, V, kScanSteps, kGated, true, true>(a, plan, s)
-                   : launch<T, V, kScanSteps, kGated, false, true>(a, plan, s);
-    return col ? launch<T, V, kScanSteps, kGated, true, false>(a, plan, s)
-               : launch<T, V, kScanSteps, kGated, false, false>(a, plan, s);
+        return col ? launch<T, V, kGated, true, true>(a, plan, s)
+                   : launch<T, V, kGated, false, true>(a, plan, s);
+    return col ? launch<T, V, kGated, true, false>(a, plan, s)
+               : launch<T, V, kGated, false, false>(a, plan, s);
+}
+
+template <typename T, int V>
+hipError_t pick(const ScanArgs &a, const ScanPlan &plan, bool gated, bool col, bool back,
+                hipStream_t s) {
+    return gated ? pick<T, V, true>(a, plan, col, back, s) : pick<T, V, false>(a, plan, col, back, s);
 }
 
 template <typename T>
 hipError_t run(const ScanArgs &a, const ScanPlan &plan, bool gated, bool col, bool back,
                hipStream_t s) {
-    hipError_t e;
-    if (plan.vec == 2)
-        e = gated ? pick<T, 2, true>(a, plan, col, back, s) : pick<T, 2, false>(a, plan, col, back, s);
-    else
-        e = gated ? pick<T, 1, true>(a, plan, col, back, s) : pick<T, 1, false>(a, plan, col, back, s);
+    const hipError_t e = plan.vec > 1 ? pick<T, kWide<T>>(a, plan, gated, col, back, s)
+                                      : pick<T, 1>(a, plan, gated, col, back, s);
     if (e != hipSuccess || !back || !col || !a.dgate) return e;
     // the workgroups' sums of a gate per value: [chunks * B][D] rows, first in runs, then all
     const int64_t m = int64_t(plan.chunks) * (a.N / a.D);
     const int D = int(a.D);
     int lanes = 1;
-    while (lanes < 64 && lanes < D) lanes *= 2;
+    while (lanes < 16 && lanes < D) lanes *= 2;
     const unsigned blocks = unsigned((D + lanes - 1) / lanes);
     const float *src = a.part;
     int64_t rows = m;
     if (plan.runs > 1) {
         const int64_t each = (m + plan.runs - 1) / plan.runs;
         float *mid = a.part + m * D;
-        hipLaunchKernelGGL((sum_rows_kernel<float>), dim3(blocks, plan.runs), dim3(256), 0, s, src,
+        hipLaunchKernelGGL((sum_rows_kernel<float>), dim3(blocks, plan.runs), dim3(1024), 0, s, src,
                            m, each, D, lanes, mid);
         src = mid;
         rows = plan.runs;
     }
-    hipLaunchKernelGGL((sum_rows_kernel<T>), dim3(blocks, 1), dim3(256), 0, s, src, rows, rows, D,
+    hipLaunchKernelGGL((sum_rows_kernel<T>), dim3(blocks, 1), dim3(1024), 0, s, src, rows, rows, D,
                        lanes, static_cast<T *>(a.dgate));
     return hipGetLastError();
 }
@@ -419,21 +579,32 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 
 }  // namespace
 
-// How the sizes are shared out.  vec: two columns a lane where every access then stays one
-// aligned word.  Waves: as many as the steps have use for.  Chunks of time: only where the
-// columns alone leave compute units idle, and of at least one tile.
-ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, bool pairs, bool col, bool back) {
-    ScanPlan plan;
+// How the sizes are shared out.  wide: columns of an 8-byte word, 1 where accesses of words would
+// not all be aligned; far: rows too far apart for a wave's addressing.
+//   A few steps, or far rows: a lane takes its columns through all of them.
+//   Else a lane takes a word of columns where that still fills the device, for its longer row
+//   segments (128 x 1024 x 256 in bf16: 42 us forward, 54 with single columns), and one column
+//   where it would not (2048 x 64 x 256: 62 us, with words 151); as many waves as the steps have use
+//   for; and chunks of time where single columns leave compute units idle and the steps are at least
+//   eight tiles (below that the second launch costs more than the idle units).
+ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int wide, bool far, bool col, bool back) {
+    ScanPlan plan{};
     const int64_t N = B * D;
-    plan.vec = pairs ? 2 : 1;
-    plan.waves = int(std::max<int64_t>(1, std::min<int64_t>(kWaves, (T + kScanSteps - 1) / kScanSteps)));
-    const int64_t tile = int64_t(plan.waves) * kScanSteps;
-    const int64_t groups = (N / plan.vec + 63) / 64;
-    const int64_t want = std::max<int64_t>(1, std::min((kFill + groups - 1) / groups,
-                                                       (T + tile - 1) / tile));
-    const int64_t tiles_each = (T + tile * want - 1) / (tile * want);
-    plan.chunk = std::max<int64_t>(1, tiles_each) * tile;
-    plan.chunks = int(std::max<int64_t>(1, (T + plan.chunk - 1) / plan.chunk));
+    plan.chunks = 1;
+    plan.chunk = std::max<int64_t>(1, T);
+    plan.vec = wide;
+    if (T >= 8 && !far) {
+        // words where they fill the device, or where chunks of time will have to anyway
+        if (N / wide < int64_t(64) * kFill && N >= int64_t(64) * kFill / 2) plan.vec = 1;
+        const int64_t K = steps_of(plan.vec), groups = scan_groups(N, plan.vec);
+        plan.waves = int(std::min<int64_t>(waves_of(plan.vec), (T + K - 1) / K));
+        const int64_t tile = plan.waves * K, tiles = (T + tile - 1) / tile;
+        const int64_t want = std::min((kFill + groups - 1) / groups, tiles);
+        if (tiles >= 4 && groups < kFill / 2) {
+            plan.chunk = (tiles + want - 1) / want * tile;
+            plan.chunks = int((T + plan.chunk - 1) / plan.chunk);
+        }
+    }
     size_t bytes = 0;
     if (plan.chunks > 1) bytes = round16(size_t(plan.chunks) * size_t(N) * sizeof(float2));
     plan.part_off = bytes;

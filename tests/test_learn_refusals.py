@@ -28,7 +28,7 @@ def scan_config(**kw):
 BAD_SCANS = [dict(steps=-1), dict(steps=1 << 31), dict(rows=-1), dict(width=0),
              dict(rows=1 << 16, width=1 << 15), dict(rows=1 << 40, width=1 << 40), dict(dtype=3),
              dict(dtype=-1), dict(form=2), dict(reverse=2), dict(gate_per_value=-1),
-             dict(x_step=1 << 60)]
+             dict(x_step=1 << 60), dict(x_row=-8), dict(gate_step=-16)]
 
 
 @pytest.mark.parametrize("bad", BAD_SCANS + [dict(y_step=0), dict(y_row=7), dict(y_step=4)])
@@ -93,7 +93,7 @@ def tokens_config(**kw):
 
 
 BAD_TOKENS = [dict(rows=-1), dict(rows=1 << 31), dict(choices=0), dict(choices=(1 << 31) - 1024),
-              dict(dtype=3), dict(ids_type=3), dict(ids_type=-1), dict(row_stride=1 << 60)]
+              dict(dtype=3), dict(ids_type=3), dict(ids_type=-1), dict(row_stride=1 << 60), dict(row_stride=-5)]
 
 
 @pytest.mark.parametrize("bad", BAD_TOKENS)
