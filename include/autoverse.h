@@ -509,6 +509,10 @@ typedef struct {
 } av_tokens_config;
 #define AV_TOP_MAX 32
 
+/* Bytes of device memory (*bytes, may be 0) that av_log_probs uses as workspace for these sizes.
+ * Host only. */
+av_status av_log_probs_workspace(const av_tokens_config *cfg, size_t *bytes);
+
 /* Log-probabilities of given tokens under softmax(logits), the entropy, and the most likely
  * alternatives (policy gradients, behaviour cloning and scoring, paper Sec. 2.3).
  *   ids       device [N] (ids_type) or NULL with logp NULL.  A number outside [0, A) is padding:
@@ -520,10 +524,12 @@ typedef struct {
  *             the lowest index first; with top = 0 not used, else neither may be NULL.
  * A logit of -infinity is a masked choice: probability 0, no part in entropy or alternatives
  * (places left over get id -1 and -infinity).  A row without any other has logp -infinity,
- * entropy 0.  A row holding a NaN or +infinity has NaN results and ids -1. */
+ * entropy 0.  A row holding a NaN or +infinity has NaN results and ids -1.
+ * workspace: av_log_probs_workspace bytes or more, 16-byte aligned, not shared by calls that may
+ * overlap; NULL where that is 0 (it is for all but a few long rows). */
 av_status av_log_probs(const av_tokens_config *cfg, const void *logits, const void *ids,
                        float *logp, float *entropy, float *stats, float *top_logp,
-                       int32_t *top_ids);
+                       int32_t *top_ids, void *workspace, size_t workspace_bytes);
 
 /* Gradient of av_log_probs: with p = softmax(logits) and the entropy H,
  *   dlogits_i = dlogp ([i = id] - p_i) - dentropy p_i (log p_i + H)

@@ -41,7 +41,7 @@ ABI_SYMBOLS = ("av_create_batch", "av_load_rules", "av_set_rule_control", "av_re
                "av_mutate_maps", "av_mutate_rules", "av_search_create", "av_search_load_rules",
                "av_search_begin", "av_search_expand", "av_search_frontier", "av_search_destroy",
                "av_step_n_static", "av_scan_workspace", "av_scan", "av_scan_backward",
-               "av_log_probs", "av_log_probs_backward", "av_draw_actions", "av_last_error")
+               "av_log_probs_workspace", "av_log_probs", "av_log_probs_backward", "av_draw_actions", "av_last_error")
 
 
 class av_config(ctypes.Structure):
@@ -168,7 +168,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "av_scan_workspace": ([P, I32, ctypes.POINTER(SZ)], ctypes.c_int),
         "av_scan": ([P] * 8 + [SZ], ctypes.c_int),
         "av_scan_backward": ([P] * 12 + [SZ], ctypes.c_int),
-        "av_log_probs": ([P] * 8, ctypes.c_int),
+        "av_log_probs_workspace": ([P, ctypes.POINTER(SZ)], ctypes.c_int),
+        "av_log_probs": ([P] * 9 + [SZ], ctypes.c_int),
         "av_log_probs_backward": ([P] * 8, ctypes.c_int),
         "av_draw_actions": ([P] * 5, ctypes.c_int),
         "av_last_error": ([], ctypes.c_char_p),
@@ -520,13 +521,15 @@ def av_scan_workspace(steps, rows, width, gate_per_value=False, backward=False) 
     return n.value
 
 
-def _workspace(lib, c, ref, backward, workspace, device):
+def _workspace(size_of, name, args, workspace, device):
     """The workspace's tensor (kept alive by the caller), address and size: the caller's, or a
     new one from torch's allocator on the current stream."""
     torch = _types()[2]
     if workspace is None:
         n = ctypes.c_size_t(0)
-        _check("av_scan_workspace", lib.av_scan_workspace(ref, backward, ctypes.byref(n)))
+        rc = size_of(*args, ctypes.byref(n))
+        if rc:
+            _check(name, rc)
         if n.value == 0:
             return None, None, 0
         workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
@@ -550,7 +553,8 @@ def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=Fal
     ph = _packed(h0, "h0", f32, shape[1:], device)
     pl = _packed(last, "last", f32, shape[1:], device)
     ref = ctypes.byref(c)
-    keep, pw, n = _workspace(lib, c, ref, 0, workspace, device)
+    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", (ref, 0), workspace,
+                             device)
     rc = lib.av_scan(ref, px, pg, pc, ph, py, pl, pw, n)
     if rc:
         _check("av_scan", rc)
@@ -579,7 +583,8 @@ def av_scan_backward(x, gate, y, dy, dx, dgate=None, h0=None, dlast=None, dh0=No
     pdl = _packed(dlast, "dlast", f32, shape[1:], device)
     pdh = _packed(dh0, "dh0", f32, shape[1:], device)
     ref = ctypes.byref(c)
-    keep, pw, n = _workspace(lib, c, ref, 1, workspace, device)
+    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", (ref, 1), workspace,
+                             device)
     rc = lib.av_scan_backward(ref, px, pg, pc, ph, py, pdy, pdl, pdx, pdg, pdh, pw, n)
     if rc:
         _check("av_scan_backward", rc)
@@ -605,8 +610,18 @@ def _tokens_config(logits, ids):
     return c, pl, pi
 
 
+def av_log_probs_workspace(rows, choices, top=0, dtype=AV_F32) -> int:
+    """Bytes of workspace av_log_probs uses for these sizes (dtype: AV_F32, AV_F16 or AV_BF16)."""
+    c = av_tokens_config()
+    c.rows, c.choices, c.top, c.dtype = rows, choices, top, dtype
+    n = ctypes.c_size_t(0)
+    _check("av_log_probs_workspace",
+           load_library().av_log_probs_workspace(ctypes.byref(c), ctypes.byref(n)))
+    return n.value
+
+
 def av_log_probs(logits, ids=None, logp=None, entropy=None, stats=None, top_logp=None,
-                 top_ids=None):
+                 top_ids=None, workspace=None):
     """Log-probabilities of the given tokens.  logits: device tensor [N][A]; ids: uint8, int32 or
     int64 [N] (outside [0, A): padding); logp, entropy: float32 [N]; stats: float32 [N][2], for
     av_log_probs_backward; top_logp, top_ids: float32 / int32 [N][k], the k <= 32 most likely.
@@ -625,7 +640,10 @@ def av_log_probs(logits, ids=None, logp=None, entropy=None, stats=None, top_logp
               _packed(top_ids, "top_ids", torch.int32, (N, c.top), device)]
     else:
         p += [None, None]
-    rc = load_library().av_log_probs(ctypes.byref(c), pl, pi, *p)
+    lib, ref = load_library(), ctypes.byref(c)
+    keep, pw, n = _workspace(lib.av_log_probs_workspace, "av_log_probs_workspace", (ref,),
+                             workspace, device)
+    rc = lib.av_log_probs(ref, pl, pi, *p, pw, n)
     if rc:
         _check("av_log_probs", rc)
 

@@ -328,7 +328,7 @@ hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool 
 
 struct TokenArgs {
     int64_t N, stride, dstride;       // rows, and the rows' strides in elements
-    int A, top, ids_type;
+    int A, top, ids_type, parts;
     const void *logits, *ids;
     float *logp, *entropy, *stats, *top_logp;
     int32_t *top_ids;
@@ -336,7 +336,14 @@ struct TokenArgs {
     void *dlogits;
     const float *uniform;
     uint8_t *actions;
+    void *part_stats;                 // parts > 1: [N][parts] sums, and [N][parts][top] keys
+    uint64_t *part_keys;
 };
+struct TokenPlan {
+    int parts;                        // workgroups that share a row
+    size_t keys_off, bytes;           // workspace: the parts' sums, then their alternatives
+};
+TokenPlan tokens_plan(int64_t N, int64_t A, int top, int dtype);
 hipError_t launch_log_probs(const TokenArgs &a, int dtype, hipStream_t s);
 hipError_t launch_log_probs_backward(const TokenArgs &a, int dtype, hipStream_t s);
 hipError_t launch_draw(const TokenArgs &a, int dtype, hipStream_t s);

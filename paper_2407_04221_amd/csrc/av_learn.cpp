@@ -101,6 +101,14 @@ bool whole(const Place &a, size_t size, int n) {
     return reinterpret_cast<uintptr_t>(a.p) % (n * size) == 0 && a.step % n == 0 && a.row % n == 0;
 }
 
+av_status check_workspace(const void *workspace, size_t bytes, size_t needed) {
+    if (needed == 0) return AV_OK;
+    if (!workspace || bytes < needed)
+        return bad("workspace of %zu bytes; %zu are needed", workspace ? bytes : size_t(0), needed);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16) return bad("workspace is not 16-byte aligned");
+    return AV_OK;
+}
+
 size_t workspace_of(const av_scan_config &c, bool back) {
     size_t most = 0;
     for (int wide : {1, int(8 / size_of(c.dtype))})
@@ -157,11 +165,9 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
         if (a.p) far = far || span * a.row + c.width >= (int64_t(1) << 32) / int64_t(size);
 
     ScanPlan plan = scan_plan(c.steps, c.rows, c.width, wide, far, col, back);
-    if (some && workspace_of(c, back) > 0) {
-        if (!workspace || workspace_bytes < workspace_of(c, back))
-            return bad("workspace of %zu bytes; %zu are needed", workspace ? workspace_bytes : 0,
-                       workspace_of(c, back));
-        if (reinterpret_cast<uintptr_t>(workspace) % 16) return bad("workspace is not 16-byte aligned");
+    if (some) {
+        if (av_status st = check_workspace(workspace, workspace_bytes, workspace_of(c, back)))
+            return st;
     }
 
     // processing order: the gradient runs against the recurrence
@@ -209,6 +215,11 @@ av_status check_tokens(const av_tokens_config *c) {
     if (!reachable(c->row_stride, c->rows)) return bad("row_stride is out of range");
     if (c->ids_type != AV_IDS_U8 && c->ids_type != AV_IDS_I32 && c->ids_type != AV_IDS_I64)
         return bad("unknown ids_type %d", c->ids_type);
+    return AV_OK;
+}
+
+av_status check_top(const av_tokens_config *c) {
+    if (c->top < 0 || c->top > AV_TOP_MAX) return bad("top %d outside [0, %d]", c->top, AV_TOP_MAX);
     return AV_OK;
 }
 
@@ -260,13 +271,21 @@ av_status av_scan_backward(const av_scan_config *cfg, const void *x, const void 
                 true);
 }
 
-av_status av_log_probs(const av_tokens_config *cfg, const void *logits, const void *ids,
-                       float *logp, float *entropy, float *stats, float *top_logp,
-                       int32_t *top_ids) {
+av_status av_log_probs_workspace(const av_tokens_config *cfg, size_t *bytes) {
     set_error(AV_OK, "");
     if (av_status st = check_tokens(cfg)) return st;
-    if (cfg->top < 0 || cfg->top > AV_TOP_MAX)
-        return bad("top %d outside [0, %d]", cfg->top, AV_TOP_MAX);
+    if (av_status st = check_top(cfg)) return st;
+    if (!bytes) return bad("bytes is NULL");
+    *bytes = tokens_plan(cfg->rows, cfg->choices, cfg->top, cfg->dtype).bytes;
+    return AV_OK;
+}
+
+av_status av_log_probs(const av_tokens_config *cfg, const void *logits, const void *ids,
+                       float *logp, float *entropy, float *stats, float *top_logp,
+                       int32_t *top_ids, void *workspace, size_t workspace_bytes) {
+    set_error(AV_OK, "");
+    if (av_status st = check_tokens(cfg)) return st;
+    if (av_status st = check_top(cfg)) return st;
     if (cfg->rows == 0) return AV_OK;
     if (!logits) return bad("logits is NULL");
     if ((logp != nullptr) != (ids != nullptr)) return bad("logp and ids go together");
@@ -275,8 +294,15 @@ av_status av_log_probs(const av_tokens_config *cfg, const void *logits, const vo
         !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(stats, 8) || !aligned(top_logp, 4) ||
         !aligned(top_ids, 4))
         return bad("a tensor is not aligned to its type (stats: 8 bytes)");
+    const TokenPlan plan = tokens_plan(cfg->rows, cfg->choices, cfg->top, cfg->dtype);
+    if (plan.bytes > 0) {
+        if (av_status st = check_workspace(workspace, workspace_bytes, plan.bytes)) return st;
+    }
     TokenArgs a = token_args(*cfg, logits, ids);
     a.top = cfg->top;
+    a.parts = plan.parts;
+    a.part_stats = workspace;
+    a.part_keys = reinterpret_cast<uint64_t *>(static_cast<char *>(workspace) + plan.keys_off);
     a.logp = logp; a.entropy = entropy; a.stats = stats;
     a.top_logp = top_logp; a.top_ids = top_ids;
     OnDevice on(cfg->device);

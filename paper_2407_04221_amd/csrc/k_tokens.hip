@@ -55,27 +55,44 @@ __device__ inline void add(Stat &a, float l) {
     a.w = fmaf(fmaxf(t, -1.0e4f), e, a.w);
 }
 
-__device__ inline void join(Stat &a, Stat b) {
-    const float m = fmaxf(a.m, b.m);
-    raise(a, m);
-    raise(b, m);
-    a.s += b.s;
-    a.w += b.w;
+// Reductions over a wave by DPP: within rows of 16 lanes, then lane 15 of a row into the next and
+// lane 31 into the upper half; lane 63 holds the result, which all lanes get.
+template <int kCtrl, int kRows> __device__ inline uint32_t from_lane(uint32_t x, uint32_t none) {
+    return uint32_t(__builtin_amdgcn_update_dpp(int(none), int(x), kCtrl, kRows, 0xF, false));
+}
+template <typename Op> __device__ inline uint32_t over_wave(uint32_t x, uint32_t none, Op op) {
+    x = op(x, from_lane<0x111, 0xF>(x, none));        // row_shr:1, 2, 4, 8
+    x = op(x, from_lane<0x112, 0xF>(x, none));
+    x = op(x, from_lane<0x114, 0xF>(x, none));
+    x = op(x, from_lane<0x118, 0xF>(x, none));
+    x = op(x, from_lane<0x142, 0xA>(x, none));        // row_bcast:15 into rows 1 and 3
+    x = op(x, from_lane<0x143, 0xC>(x, none));        // row_bcast:31 into rows 2 and 3
+    return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
+}
+__device__ inline float wave_max(float v) {
+    return __uint_as_float(over_wave(__float_as_uint(v), __float_as_uint(kNone),
+                                     [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+__device__ inline float wave_sum(float v) {
+    return __uint_as_float(over_wave(__float_as_uint(v), 0u, [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+__device__ inline uint32_t wave_max(uint32_t v) {
+    return over_wave(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ inline uint64_t wave_max(uint64_t k) {
+    const uint32_t hi = wave_max(uint32_t(k >> 32));
+    return uint64_t(hi) << 32 | wave_max(uint32_t(k >> 32) == hi ? uint32_t(k) : 0u);
 }
 
-template <int kLanes> __device__ inline Stat join_lanes(Stat a) {
-#pragma unroll
-    for (int d = kLanes / 2; d > 0; d >>= 1) {
-        Stat b;
-        b.m = __shfl_xor(a.m, d);
-        b.s = __shfl_xor(a.s, d);
-        b.w = __shfl_xor(a.w, d);
-        // both lanes of a pair add the same two parts in the same order
-        const bool low = (threadIdx.x & d) == 0;
-        Stat x = low ? a : b;
-        join(x, low ? b : a);
-        a = x;
-    }
+// The sum of the lanes' sets: all are raised to the largest maximum and added.
+__device__ inline Stat join_lanes(Stat a) {
+    raise(a, wave_max(a.m));
+    a.s = wave_sum(a.s);
+    a.w = wave_sum(a.w);
     return a;
 }
 
@@ -104,15 +121,6 @@ __device__ inline uint64_t key_of(float l, int i) {
 __device__ inline float key_logit(uint64_t k) {
     const uint32_t u = uint32_t(k >> 32);
     return __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
-}
-
-__device__ inline uint64_t max_lanes(uint64_t k) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const uint64_t o = __shfl_xor(static_cast<unsigned long long>(k), d);
-        k = o > k ? o : k;
-    }
-    return k;
 }
 
 __device__ inline void put_top(const TokenArgs &a, const Row &r, int64_t row, int j, uint64_t k) {
@@ -274,10 +282,35 @@ template <int kPer> __device__ inline uint64_t best_key(const float (&v)[kPer], 
     return k;
 }
 
-// One wave per row of at most kWaveRow choices, held in registers.
+// The k-th largest of the wave's 64 numbers (0 if fewer are set): bit by bit from the top, the
+// largest number that k of them reach.
+__device__ inline uint32_t kth_of_wave(uint32_t x, int k) {
+    uint32_t t = 0;
+#pragma unroll 4
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t up = t | 1u << bit;
+        if (__popcll(__ballot(x >= up)) >= k) t = up;
+    }
+    return t;
+}
+// The same of keys; the lower halves are only looked at where the upper ones leave a tie.
+__device__ inline uint64_t kth_of_wave(uint64_t key, int k) {
+    const uint32_t hi = uint32_t(key >> 32), t = kth_of_wave(hi, k);
+    const int above = __popcll(__ballot(hi > t)), equal = __popcll(__ballot(hi == t));
+    if (t == 0 || above + equal == k) return uint64_t(t) << 32;
+    return uint64_t(t) << 32 | kth_of_wave(hi == t ? uint32_t(key) : 0u, k - above);
+}
+
+constexpr int kWaveList = 256;       // candidates for the alternatives of a wave's row
+
+// One wave per row of at most kWaveRow choices, held in registers.  Alternatives: no one is smaller
+// than the k-th largest of the lanes' maxima; the elements that reach it are listed in LDS, and a
+// listed key's place is the number of larger ones.  Where they are too many (equal elements, or few
+// choices left), the largest key below the last is taken again and again.
 template <typename T, int kWords>
 __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
+    __shared__ unsigned long long lists[4][kWaveList];
     const int lane = threadIdx.x & 63;
     const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= a.N) return;
@@ -285,115 +318,340 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     float v[kWords][kPer];
 #pragma unroll
     for (int j = 0; j < kWords; ++j) in.load(j * 64 + lane, v[j]);
-    Stat st{kNone, 0.0f, 0.0f};
+    float m = kNone;
 #pragma unroll
-    for (int j = 0; j < kWords; ++j) st.m = fmaxf(st.m, largest(v[j]));
+    for (int j = 0; j < kWords; ++j) m = fmaxf(m, largest(v[j]));
+    Stat st{wave_max(m), 0.0f, 0.0f};
 #pragma unroll
     for (int j = 0; j < kWords; ++j)
 #pragma unroll
         for (int i = 0; i < kPer; ++i) add(st, v[j][i]);
-    st = join_lanes<64>(st);
+    st.s = wave_sum(st.s);
+    st.w = wave_sum(st.w);
     const Row r = row_of(st);
     if (lane == 0) put_row(a, r, row, in.l);
-    if (a.top) {
-        uint64_t last = ~uint64_t(0);
-        for (int n = 0; n < a.top; ++n) {
-            uint64_t best = 0;
+    if (a.top == 0) return;
+    unsigned long long *list = lists[threadIdx.x >> 6];
+    const uint64_t bound = uint64_t(kth_of_wave(uint32_t(key_of(m, 0) >> 32), a.top)) << 32;
+    const float least = bound == 0 ? -__FLT_MAX__ : key_logit(bound);
+    int n = 0;
 #pragma unroll
-            for (int j = 0; j < kWords; ++j)
+    for (int j = 0; j < kWords; ++j)
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const uint64_t k = key_of(v[j][i], in.first(j * 64 + lane) + i);
-                    if (k < last && k > best) best = k;
-                }
-            best = max_lanes(best);
-            if (lane == 0) put_top(a, r, row, n, best);
-            last = best;
+        for (int i = 0; i < kPer; ++i) {
+            const uint64_t who = __ballot(v[j][i] >= least);
+            const int at = n + int(__builtin_amdgcn_mbcnt_hi(uint32_t(who >> 32),
+                                   __builtin_amdgcn_mbcnt_lo(uint32_t(who), 0u)));
+            if (v[j][i] >= least && at < kWaveList)
+                list[at] = key_of(v[j][i], in.first(j * 64 + lane) + i);
+            n += __popcll(who);
         }
+    if (n <= kWaveList) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        for (int i = lane; i < n; i += 64) {
+            const uint64_t k = list[i];
+            int place = 0;
+            for (int j = 0; j < n; ++j) place += list[j] > k;
+            if (place < a.top) put_top(a, r, row, place, k);
+        }
+        for (int j = n + lane; j < a.top; j += 64) put_top(a, r, row, j, 0);
+        return;
+    }
+    uint64_t last = ~uint64_t(0);
+    for (int t = 0; t < a.top; ++t) {
+        uint64_t next = 0;
+#pragma unroll
+        for (int j = 0; j < kWords; ++j)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const uint64_t k = key_of(v[j][i], in.first(j * 64 + lane) + i);
+                if (k < last && k > next) next = k;
+            }
+        next = wave_max(next);
+        if (lane == 0) put_top(a, r, row, t, next);
+        last = next;
     }
 }
 
-// One workgroup per row of any length.
-template <typename T, int kThreads>
+// Stores a word past the caches: the gradient is not read again here, and the logits, which the
+// forward pass has just read, stay (4096 x 32768 in bf16, both passes: 169 us, so 142).
+template <typename T, int n> __device__ inline void put_past(T *to, const Vec<T, n> &v) {
+    static_assert(sizeof v == 16, "one word");
+    typedef uint32_t Word __attribute__((ext_vector_type(4)));
+    Word u;
+    __builtin_memcpy(&u, &v, 16);
+    __builtin_nontemporal_store(u, reinterpret_cast<Word *>(to));
+}
+
+// The whole words of a row, and the elements before and after them, which the first 2 kPer threads
+// take one by one (head, then tail); or one part of `parts` of them: the words from..to - 1, the
+// head with the first part and the tail with the last.
+template <typename T> struct Parts {
+    static constexpr int kPer = 16 / sizeof(T);
+    const T *l;
+    int head, words, tail, from, to;
+
+    __device__ Parts(const TokenArgs &a, int64_t row, int part = 0, int parts = 1)
+        : l(static_cast<const T *>(a.logits) + row * a.stride) {
+        head = min(a.A, int(-(reinterpret_cast<uintptr_t>(l) / sizeof(T)) % kPer));
+        words = (a.A - head) / kPer;
+        tail = a.A - head - words * kPer;
+        const int each = (words + parts - 1) / parts;
+        from = min(words, part * each);
+        to = min(words, from + each);
+        if (part > 0) head_of = 0;
+        if (part < parts - 1) tail_of = 0;
+    }
+    int head_of = 1 << 30, tail_of = 1 << 30;        // limits on the ends this part takes
+    __device__ Vec<T, kPer> word(int w) const {
+        return reinterpret_cast<const Vec<T, kPer> *>(l + head)[w];
+    }
+    __device__ int first(int w) const { return head + w * kPer; }
+    // The single element of a thread: its index, or -1.
+    __device__ int single(int tid, bool after) const {
+        if (after) {
+            const int i = tid - kPer;
+            return i >= 0 && i < min(tail, tail_of) ? head + words * kPer + i : -1;
+        }
+        return tid < min(head, head_of) ? tid : -1;
+    }
+};
+
+constexpr int kList = 2048;          // candidates for the alternatives
+
+// Alternatives of a row; m is the largest of the thread's own elements.
+//
+// Where k threads of one wave hold an element of at least x, no alternative is smaller than x.  The
+// largest such bound over the waves leaves a few k threads with a larger element; all threads share
+// those threads' words, list what reaches the bound, and a listed key's place is the number of larger
+// ones.  Where the list is too small because many elements are equal, the bound is taken over keys,
+// which also tell equal elements apart; where it still is (thousands of the largest in a few
+// threads' hands, or fewer than k choices in any wave), the alternatives are found one after another,
+// each in a pass over the row.
+//
+// put(place, key) takes them; a key of 0 says that there is none.
+template <typename T, int kThreads, typename Put>
+__device__ void alternatives(const TokenArgs &a, const Parts<T> &in, float m, Put put) {
+    constexpr int kPer = Parts<T>::kPer, kWaves = kThreads / 64;
+    __shared__ unsigned long long list[kList], keys[kWaves];
+    __shared__ uint16_t holders[kThreads];
+    __shared__ int listed, held;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int each = (in.to - in.from + kThreads - 1) / kThreads;     // words of a thread
+    uint64_t best = key_of(m, 0);                              // at least any key of the thread's
+    for (int exact = 0; exact < 2; ++exact) {
+        if (exact) {
+            best = 0;
+            for (int after = 0; after < 2; ++after) {
+                const int i = in.single(tid, after);
+                if (i >= 0) best = max(best, key_of(to_f32(in.l[i]), i));
+            }
+            for (int word = in.from + tid; word < in.to; word += kThreads) {
+                const Vec<T, kPer> q = in.word(word);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (to_f32(q.v[i]) == m) best = max(best, key_of(m, in.first(word) + i));
+            }
+        }
+        const uint64_t mine = exact ? kth_of_wave(best, a.top)
+                                    : uint64_t(kth_of_wave(uint32_t(best >> 32), a.top)) << 32;
+        __syncthreads();
+        if (lane == 0) keys[w] = mine;
+        if (tid == 0) listed = held = 0;
+        __syncthreads();
+        uint64_t bound = 1;                           // a masked choice's key is 0
+        for (int j = 0; j < kWaves; ++j) bound = max(bound, uint64_t(keys[j]));
+        if (best >= bound) holders[atomicAdd(&held, 1)] = uint16_t(tid);
+        __syncthreads();
+        auto offer = [&](float v, int i) {
+            const uint64_t k = key_of(v, i);
+            if (k < bound) return;
+            const int at = atomicAdd(&listed, 1);
+            if (at < kList) list[at] = k;
+        };
+        for (int after = 0; after < 2; ++after) {
+            const int i = in.single(tid, after);
+            if (i >= 0) offer(to_f32(in.l[i]), i);
+        }
+        const int tasks = held * each;
+        for (int t = tid; t < tasks; t += kThreads) {
+            const int word = in.from + holders[t / each] + t % each * kThreads;
+            if (word >= in.to) continue;
+            const Vec<T, kPer> q = in.word(word);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) offer(to_f32(q.v[i]), in.first(word) + i);
+        }
+        __syncthreads();
+        const int n = listed;
+        if (n > kList) continue;
+        for (int i = tid; i < n; i += kThreads) {
+            const uint64_t k = list[i];
+            int place = 0;
+            for (int j = 0; j < n; ++j) place += list[j] > k;
+            if (place < a.top) put(place, k);
+        }
+        for (int j = n + tid; j < a.top; j += kThreads) put(j, uint64_t(0));
+        return;
+    }
+    uint64_t last = ~uint64_t(0);
+    for (int j = 0; j < a.top; ++j) {
+        uint64_t next = 0;
+        auto look = [&](float v, int i) {
+            const uint64_t k = key_of(v, i);
+            if (k < last && k > next) next = k;
+        };
+        for (int after = 0; after < 2; ++after) {
+            const int i = in.single(tid, after);
+            if (i >= 0) look(to_f32(in.l[i]), i);
+        }
+        for (int word = in.from + tid; word < in.to; word += kThreads) {
+            const Vec<T, kPer> q = in.word(word);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) look(to_f32(q.v[i]), in.first(word) + i);
+        }
+        next = wave_max(next);
+        __syncthreads();
+        if (lane == 0) keys[w] = next;
+        __syncthreads();
+        for (int i = 0; i < kWaves; ++i) next = max(next, uint64_t(keys[i]));
+        if (tid == 0) put(j, next);
+        last = next;
+    }
+}
+
+// One workgroup per row of any length, or, kSplit, per part of it (blockIdx.y), whose sums and
+// alternatives go to the workspace.  A thread has kWords 16-byte words on their way at once; the
+// largest of their elements is found first, so that the sums are rescaled at most once for all.
+template <typename T, int kThreads, int kWords, bool kSplit>
 __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
-    constexpr int kPer = Words<T>::kPer, kWaves = kThreads / 64;
+    constexpr int kPer = Parts<T>::kPer, kWaves = kThreads / 64;
     __shared__ Stat stats[kWaves];
-    __shared__ unsigned long long keys[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t row = blockIdx.x;
-    const Words<T> in(a, row);
-    Stat st{kNone, 0.0f, 0.0f};
-    uint64_t best = 0;
-    for (int word = tid; word < in.count; word += kThreads) {
-        float v[kPer];
-        in.load(word, v);
-        const float m = largest(v);
-        if (m > st.m) {                               // the first of equal ones stays the best
-            if (a.top) best = best_key(v, in.first(word));
-            raise(st, m);
-        }
+    const Parts<T> in(a, row, kSplit ? blockIdx.y : 0, kSplit ? a.parts : 1);
+    // the row's ends
+    const int before = in.single(tid, false), after = in.single(tid, true);
+    const float va = before >= 0 ? to_f32(in.l[before]) : kNone;
+    const float vb = after >= 0 ? to_f32(in.l[after]) : kNone;
+    Stat st{fmaxf(va, vb), 0.0f, 0.0f};
+    add(st, va);
+    add(st, vb);
+    for (int word = in.from + tid; word < in.to; word += kWords * kThreads) {
+        Vec<T, kPer> q[kWords];
+        const bool whole = word + (kWords - 1) * kThreads < in.to;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) add(st, v[i]);
+        for (int j = 0; j < kWords; ++j)               // past the end: the last word again
+            q[j] = in.word(whole ? word + j * kThreads : min(word + j * kThreads, in.to - 1));
+        float m = st.m;
+#pragma unroll
+        for (int j = 0; j < kWords; ++j)
+            if (whole || word + j * kThreads < in.to) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) m = fmaxf(m, to_f32(q[j].v[i]));
+            }
+        if (m > st.m) raise(st, m);
+#pragma unroll
+        for (int j = 0; j < kWords; ++j)
+            if (whole || word + j * kThreads < in.to) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) add(st, to_f32(q[j].v[i]));
+            }
     }
-    st = join_lanes<64>(st);
+    const float mine = st.m;
+    st = join_lanes(st);
     if (lane == 0) stats[w] = st;
     __syncthreads();
-    st = stats[0];
-    for (int j = 1; j < kWaves; ++j) join(st, stats[j]);
-    const Row r = row_of(st);
-    if (tid == 0) put_row(a, r, row, in.l);
-    // alternatives one after another: the best of the threads' best; the wave that held it
-    // finds its thread's next in that thread's words
-    for (int n = 0; n < a.top; ++n) {
-        const uint64_t mine = max_lanes(best);
-        if (lane == 0) keys[w] = mine;
-        __syncthreads();
-        uint64_t top = keys[0];
-        for (int j = 1; j < kWaves; ++j) top = keys[j] > top ? keys[j] : top;
-        if (tid == 0) put_top(a, r, row, n, top);
-        if (top != 0 && mine == top) {
-            const int owner = __ffsll(__ballot(best == top)) - 1;
-            uint64_t next = 0;
-            for (int word = w * 64 + owner + lane * kThreads; word < in.count;
-                 word += 64 * kThreads) {
-                float v[kPer];
-                in.load(word, v);
-#pragma unroll
-                for (int i = 0; i < kPer; ++i) {
-                    const uint64_t k = key_of(v[i], in.first(word) + i);
-                    if (k < top && k > next) next = k;
-                }
-            }
-            next = max_lanes(next);
-            if (lane == owner) best = next;
+    Stat all{kNone, 0.0f, 0.0f};
+    if (lane < kWaves) all = stats[lane];
+    all = join_lanes(all);
+    if (kSplit) {
+        const int64_t at = row * a.parts + blockIdx.y;
+        if (tid == 0) static_cast<Stat *>(a.part_stats)[at] = all;
+        if (a.top) {
+            uint64_t *keys = a.part_keys + at * a.top;
+            alternatives<T, kThreads>(a, in, mine, [&](int place, uint64_t k) { keys[place] = k; });
         }
-        __syncthreads();
+        return;
     }
+    const Row r = row_of(all);
+    if (tid == 0) put_row(a, r, row, in.l);
+    if (a.top)
+        alternatives<T, kThreads>(a, in, mine, [&](int place, uint64_t k) {
+            put_top(a, r, row, place, k);
+        });
+}
+
+// The rows from their parts (at most 64).  The parts' alternatives are in falling order, so a key's
+// place is the sum over the parts of how many there are larger, each found by bisection.
+template <typename T> __global__ void __launch_bounds__(256) join_rows_kernel(TokenArgs a) {
+    __shared__ uint64_t keys[64 * AV_TOP_MAX];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int64_t row = blockIdx.x;
+    Stat all{kNone, 0.0f, 0.0f};
+    if (lane < a.parts) all = static_cast<const Stat *>(a.part_stats)[row * a.parts + lane];
+    const Row r = row_of(join_lanes(all));
+    if (tid == 0) put_row(a, r, row, static_cast<const T *>(a.logits) + row * a.stride);
+    if (a.top == 0) return;
+    const int n = a.parts * a.top;
+    for (int i = tid; i < n; i += 256) keys[i] = a.part_keys[row * n + i];
+    __syncthreads();
+    // larger keys than k in a part's falling list
+    auto larger = [&](int part, uint64_t k) {
+        int lo = 0, hi = a.top;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (keys[part * a.top + mid] > k) lo = mid + 1;
+            else hi = mid;
+        }
+        return lo;
+    };
+    for (int i = tid; i < n; i += 256) {
+        if (keys[i] == 0) continue;
+        int place = 0;
+        for (int p = 0; p < a.parts; ++p) place += larger(p, keys[i]);
+        if (place < a.top) put_top(a, r, row, place, keys[i]);
+    }
+    int live = 0;
+    for (int p = 0; p < a.parts; ++p) live += larger(p, 0);
+    for (int j = live + tid; j < a.top; j += 256) put_top(a, r, row, j, 0);
 }
 
 // Gradient of rows of any length; kSame: dlogits' rows are as far into a word as the logits'.
 // blockIdx.y, and the threads, share a row's words.
 template <typename T, bool kSame>
-__global__ void __launch_bounds__(256) long_back_kernel(TokenArgs a, int per_row) {
-    constexpr int kPer = Words<T>::kPer;
+__global__ void __launch_bounds__(256) long_back_kernel(TokenArgs a) {
+    constexpr int kPer = Parts<T>::kPer;
     const int64_t row = blockIdx.x;
-    const Words<T> in(a, row);
+    const Parts<T> in(a, row);
     T *d = static_cast<T *>(a.dlogits) + row * a.dstride;
     const Back b = back_of(a, row);
-    for (int word = int(blockIdx.y) * 256 + threadIdx.x; word < in.count; word += per_row * 256) {
-        float v[kPer];
-        in.load(word, v);
+    if (blockIdx.y == 0) {
+        for (int after = 0; after < 2; ++after) {
+            const int i = in.single(threadIdx.x, after);
+            if (i < 0) continue;
+            float v[1] = {to_f32(in.l[i])};
+            slopes(b, i, v);
+            d[i] = from_f32<T>(v[0]);
+        }
+    }
+    const int stride = int(gridDim.y) * 256;
+    for (int word = int(blockIdx.y) * 256 + threadIdx.x; word < in.words; word += stride) {
+        const Vec<T, kPer> q = in.word(word);
         const int at = in.first(word);
+        float v[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[i] = to_f32(q.v[i]);
         slopes(b, at, v);
         Vec<T, kPer> o;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) o.v[i] = from_f32<T>(v[i]);
-        if (kSame && in.whole(word)) {
-            *reinterpret_cast<Vec<T, kPer> *>(d + at) = o;
+        if (kSame) {
+            put_past(d + at, o);
         } else {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (at + i >= 0 && at + i < a.A) d[at + i] = o.v[i];
+            for (int i = 0; i < kPer; ++i) d[at + i] = o.v[i];
         }
     }
 }
@@ -508,10 +766,17 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
         else hipLaunchKernelGGL((wave_rows_kernel<T, 8>), g, b, 0, s, a);
         return hipGetLastError();
     }
-    if (a.N >= 512)
-        hipLaunchKernelGGL((long_rows_kernel<T, 256>), dim3(unsigned(a.N)), b, 0, s, a);
-    else
-        hipLaunchKernelGGL((long_rows_kernel<T, 1024>), dim3(unsigned(a.N)), dim3(1024), 0, s, a);
+    const dim3 g(unsigned(a.N), unsigned(a.parts));
+    if (a.parts > 1) {
+        hipLaunchKernelGGL((long_rows_kernel<T, 256, 4, true>), g, b, 0, s, a);
+        hipLaunchKernelGGL((join_rows_kernel<T>), dim3(unsigned(a.N)), b, 0, s, a);
+    } else if (a.N >= 2048) {
+        hipLaunchKernelGGL((long_rows_kernel<T, 256, 4, false>), g, b, 0, s, a);
+    } else if (a.N >= 512) {
+        hipLaunchKernelGGL((long_rows_kernel<T, 512, 4, false>), g, dim3(512), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((long_rows_kernel<T, 1024, 4, false>), g, dim3(1024), 0, s, a);
+    }
     return hipGetLastError();
 }
 
@@ -539,8 +804,8 @@ template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
     const int per_row = int(std::max<int64_t>(1, std::min<int64_t>(blocks_of(words, 256),
                                                                    (2048 + a.N - 1) / a.N)));
     const dim3 g(unsigned(a.N), unsigned(per_row));
-    if (same) hipLaunchKernelGGL((long_back_kernel<T, true>), g, b, 0, s, a, per_row);
-    else hipLaunchKernelGGL((long_back_kernel<T, false>), g, b, 0, s, a, per_row);
+    if (same) hipLaunchKernelGGL((long_back_kernel<T, true>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((long_back_kernel<T, false>), g, b, 0, s, a);
     return hipGetLastError();
 }
 
@@ -553,6 +818,20 @@ template <typename T> hipError_t draw(const TokenArgs &a, hipStream_t s) {
 }
 
 }  // namespace
+
+// Few long rows are cut into parts, so that their exponentials (which bound a row that one compute
+// unit takes alone: 131072 choices, 12 us) are shared: up to two parts a compute unit, each of 1024
+// words or more (four a thread).
+TokenPlan tokens_plan(int64_t N, int64_t A, int top, int dtype) {
+    TokenPlan plan{1, 0, 0};
+    const int64_t words = A / (dtype == AV_F32 ? 4 : 8);
+    if (A > kWaveRow && N > 0 && N <= 256 && words >= 2048) {
+        plan.parts = int(std::min<int64_t>({64, 512 / N, words / 1024}));
+        plan.keys_off = (size_t(N) * plan.parts * sizeof(Stat) + 15) & ~size_t(15);
+        plan.bytes = plan.keys_off + size_t(N) * plan.parts * size_t(top) * sizeof(uint64_t);
+    }
+    return plan;
+}
 
 hipError_t launch_log_probs(const TokenArgs &a, int dtype, hipStream_t s) {
     switch (dtype) {

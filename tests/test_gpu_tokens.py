@@ -103,7 +103,7 @@ def test_strides(pad, shift, bpad, bshift, A, dtype):
         assert (between == 9.0).all()
 
 
-@pytest.mark.parametrize("A", [5, 100, 2000, 9000])
+@pytest.mark.parametrize("A", [5, 100, 2000, 9000, 33000])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_masks(A, dtype):
     """Masked choices, given tokens among them, and rows that a mask leaves one or no choice."""
@@ -126,7 +126,7 @@ def test_masks(A, dtype):
     assert logp[2] == -np.inf and ent[1] == 0
 
 
-@pytest.mark.parametrize("A", [3, 60, 1500, 7000])
+@pytest.mark.parametrize("A", [3, 60, 1500, 7000, 20001])
 def test_infinities_and_nan(A):
     """A row with a NaN or +inf is NaN throughout and leaves its neighbours alone."""
     logits, r = some(8, A, "f32")
@@ -172,7 +172,7 @@ def test_confident_and_wide_rows():
 
 def test_parts_on_request():
     """Any output alone, either gradient alone, and the gradient in place."""
-    for A in (5, 300, 4000):
+    for A in (5, 300, 4000, 30000):
         logits, r = some(10, A, "f32")
         ids = torch.from_numpy(r.integers(0, A, size=10)).cuda()
         f = dict(device="cuda")
@@ -234,6 +234,41 @@ def test_draw(A, dtype):
         again = torch.empty_like(actions)
         av.av_draw_actions(logits, torch.from_numpy(u).cuda(), again)
         assert torch.equal(again, actions)
+
+
+def test_long_rows_in_graphs_with_workspaces():
+    """A few long rows, whose parts meet in a workspace: two captured launches with one each."""
+    f = dict(device="cuda")
+    l = [torch.randn((3, 50000), **f) for _ in range(2)]
+    ids = torch.arange(3, **f)
+
+    def buffers():
+        return [torch.zeros(3, **f), torch.zeros(3, **f), torch.zeros((3, 2), **f),
+                torch.zeros((3, 9), **f), torch.zeros((3, 9), dtype=torch.int32, **f)]
+    want, outs, graphs = [buffers(), buffers()], [buffers(), buffers()], []
+    for v, w in zip(l, want):
+        av.av_log_probs(v, ids, *w)
+    torch.cuda.synchronize()
+    for v, o in zip(l, outs):
+        ws = torch.empty(av.av_log_probs_workspace(3, 50000, 9), dtype=torch.uint8, **f)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            av.av_log_probs(v, ids, *o, workspace=ws)
+        graphs.append((g, ws))
+    for _ in range(3):
+        for g, _ in graphs:
+            g.replay()
+        again = buffers()
+        av.av_log_probs(l[0], ids, *again)
+        torch.cuda.synchronize()
+        for o, w in zip(outs + [again], want + [want[0]]):
+            for x, y in zip(o, w):
+                assert torch.equal(x, y)
+        for o in outs:
+            for x in o:
+                x.zero_()
+    with pytest.raises(av.AvError):
+        av.av_log_probs(l[0], ids, *again, workspace=torch.empty(64, dtype=torch.uint8, **f))
 
 
 def test_draw_follows_the_distribution():

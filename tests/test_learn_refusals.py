@@ -98,7 +98,7 @@ BAD_TOKENS = [dict(rows=-1), dict(rows=1 << 31), dict(choices=0), dict(choices=(
 
 @pytest.mark.parametrize("bad", BAD_TOKENS)
 def test_tokens_refuse(lib, bad):
-    assert lib.av_log_probs(tokens_config(**bad), P, P, P, P, P, None, None) == av.AV_EINVAL
+    assert lib.av_log_probs(tokens_config(**bad), P, P, P, P, P, None, None, None, 0) == av.AV_EINVAL
     assert lib.av_log_probs_backward(tokens_config(**bad), P, P, P, P, P, P, P) == av.AV_EINVAL
     assert lib.av_draw_actions(tokens_config(**bad), P, P, P, P) == av.AV_EINVAL
     assert av.av_last_error()
@@ -107,17 +107,17 @@ def test_tokens_refuse(lib, bad):
 def test_tokens_refuse_missing_and_misaligned(lib):
     odd, four = ctypes.c_void_p(4097), ctypes.c_void_p(4100)
     cfg = tokens_config()
-    assert lib.av_log_probs(None, P, P, P, P, P, None, None) == av.AV_EINVAL
-    assert lib.av_log_probs(cfg, None, P, P, P, P, None, None) == av.AV_EINVAL
-    assert lib.av_log_probs(cfg, odd, P, P, P, P, None, None) == av.AV_EINVAL
-    assert lib.av_log_probs(cfg, P, None, P, P, P, None, None) == av.AV_EINVAL
-    assert lib.av_log_probs(cfg, P, P, None, P, P, None, None) == av.AV_EINVAL
-    assert lib.av_log_probs(cfg, P, P, P, P, four, None, None) == av.AV_EINVAL
+    assert lib.av_log_probs(None, P, P, P, P, P, None, None, None, 0) == av.AV_EINVAL
+    assert lib.av_log_probs(cfg, None, P, P, P, P, None, None, None, 0) == av.AV_EINVAL
+    assert lib.av_log_probs(cfg, odd, P, P, P, P, None, None, None, 0) == av.AV_EINVAL
+    assert lib.av_log_probs(cfg, P, None, P, P, P, None, None, None, 0) == av.AV_EINVAL
+    assert lib.av_log_probs(cfg, P, P, None, P, P, None, None, None, 0) == av.AV_EINVAL
+    assert lib.av_log_probs(cfg, P, P, P, P, four, None, None, None, 0) == av.AV_EINVAL
     for top in (-1, 33):
-        assert lib.av_log_probs(tokens_config(top=top), P, P, P, P, P, P, P) == av.AV_EINVAL
-    assert lib.av_log_probs(tokens_config(top=1), P, P, P, P, P, None, P) == av.AV_EINVAL
+        assert lib.av_log_probs(tokens_config(top=top), P, P, P, P, P, P, P, None, 0) == av.AV_EINVAL
+    assert lib.av_log_probs(tokens_config(top=1), P, P, P, P, P, None, P, None, 0) == av.AV_EINVAL
     assert lib.av_log_probs(tokens_config(ids_type=2), P, four, P, P, P, None,
-                            None) == av.AV_EINVAL
+                            None, None, 0) == av.AV_EINVAL
     good = [P, P, P, P, P, P, P]
     for i in (0, 1, 2, 3, 6):             # logits, ids, stats, entropy, dlogits
         args = list(good)
@@ -135,9 +135,26 @@ def test_tokens_refuse_missing_and_misaligned(lib):
     assert lib.av_draw_actions(tokens_config(choices=257), P, P, P, P) == av.AV_EINVAL
 
 
+def test_tokens_workspace(lib):
+    n = ctypes.c_size_t(1)
+    assert lib.av_log_probs_workspace(tokens_config(), ctypes.byref(n)) == av.AV_OK
+    assert n.value == 0
+    assert lib.av_log_probs_workspace(tokens_config(), None) == av.AV_EINVAL
+    assert lib.av_log_probs_workspace(None, ctypes.byref(n)) == av.AV_EINVAL
+    assert lib.av_log_probs_workspace(tokens_config(top=33), ctypes.byref(n)) == av.AV_EINVAL
+    few = dict(choices=100000, row_stride=100000, top=3)
+    assert lib.av_log_probs_workspace(tokens_config(**few), ctypes.byref(n)) == av.AV_OK
+    assert n.value > 0
+    assert n.value == av.av_log_probs_workspace(3, 100000, 3)
+    for ws, size in ((None, n.value), (P, n.value - 1), (ctypes.c_void_p(4104), n.value)):
+        assert lib.av_log_probs(tokens_config(**few), P, P, P, P, P, P, P, ws,
+                                size) == av.AV_EINVAL
+        assert "workspace" in av.av_last_error()
+
+
 def test_no_rows_need_nothing(lib):
     empty = tokens_config(rows=0)
-    assert lib.av_log_probs(empty, None, None, None, None, None, None, None) == av.AV_OK
+    assert lib.av_log_probs(empty, None, None, None, None, None, None, None, None, 0) == av.AV_OK
     assert lib.av_log_probs_backward(empty, None, None, None, None, None, None, None) == av.AV_OK
     assert lib.av_draw_actions(empty, None, None, None, None) == av.AV_OK
 
