@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -438,30 +439,37 @@ def av_destroy_batch(batch):
 
 # --- the learner's operators ----------------------------------------------------------------
 
-_dtypes = None
+# A call's host time is most of a small operator's cost, so arguments are checked with as few steps as
+# will do and its config struct is packed in one (the fields of av_scan_config, av_tokens_config).
+_SCAN = struct.Struct("3q4i14q2iP")
+_TOKENS = struct.Struct("2q2i2q2iP")
+_known = None
 
 
 def _types():
-    """torch's element types and token types as the library numbers them."""
-    global _dtypes
-    if _dtypes is None:
+    """torch's element types and token types as the library numbers them, and what else of torch
+    a call needs."""
+    global _known
+    if _known is None:
         torch = _torch()
-        _dtypes = ({torch.float32: AV_F32, torch.float16: AV_F16, torch.bfloat16: AV_BF16},
-                   {torch.uint8: AV_IDS_U8, torch.int32: AV_IDS_I32, torch.int64: AV_IDS_I64},
-                   torch)
-    return _dtypes
+        _known = ({torch.float32: AV_F32, torch.float16: AV_F16, torch.bfloat16: AV_BF16},
+                  {torch.uint8: AV_IDS_U8, torch.int32: AV_IDS_I32, torch.int64: AV_IDS_I64},
+                  torch, torch.Tensor, torch.float32, torch._C._cuda_getCurrentRawStream)
+    return _known
+
+
+def _check_tensor(t, name, dtype, shape, device):
+    if not isinstance(t, _known[3]):
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype is not dtype or t.shape != shape or t.device != device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _operand(t, name, dtype, shape, device):
     """The address of a device tensor of this type, shape and device whose last dimension is
-    contiguous, and its strides; (None, ...) of none."""
-    if t is None:
-        return None, (0,) * len(shape)
-    if not isinstance(t, _types()[2].Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
-    if t.dtype != dtype or t.shape != shape or t.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got "
-                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    contiguous, and its strides."""
+    _check_tensor(t, name, dtype, shape, device)
     strides = t.stride()
     if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
@@ -472,71 +480,62 @@ def _packed(t, name, dtype, shape, device):
     """The address of a contiguous device tensor of this type, shape and device, or None."""
     if t is None:
         return None
-    p, _ = _operand(t, name, dtype, shape, device)
+    _check_tensor(t, name, dtype, shape, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return p
+    return t.data_ptr()
 
 
-def _scan_config(x, gate, cut, form, reverse):
-    floats, _, torch = _types()
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in floats:
-        raise TypeError("x must be a float32, float16 or bfloat16 device tensor [T][B][D]")
-    shape, device, dtype = x.shape, x.device, x.dtype
-    T, B, D = shape
-    if B == 0 or D == 0:
-        raise ValueError(f"an empty recurrence: x has shape {tuple(shape)}")
-    c = av_scan_config()
-    c.steps, c.rows, c.width, c.dtype = T, B, D, floats[dtype]
-    c.form = SCAN_FORMS[form] if isinstance(form, str) else int(form)
-    c.reverse = 1 if reverse else 0
-    px, s = _operand(x, "x", dtype, shape, device)
-    c.x_step, c.x_row = s[0], s[1]
-    if gate.dim() == 1:
-        c.gate_per_value = 1
-        pg, _ = _operand(gate, "gate", dtype, shape[2:], device)
-    else:
-        pg, s = _operand(gate, "gate", dtype, shape, device)
-        c.gate_step, c.gate_row = s[0], s[1]
-    pc = None
-    if cut is not None:
-        if not isinstance(cut, torch.Tensor) or not cut.is_cuda:
-            raise TypeError("cut must be a device tensor")
-        if cut.dtype != torch.uint8 or cut.shape != shape[:2] or cut.device != device:
-            raise ValueError(f"cut must be a uint8 tensor of shape {tuple(shape[:2])} on {device}")
-        pc = cut.data_ptr()
-        c.cut_step, c.cut_row = cut.stride()
-    c.device = device.index
-    c.stream = torch.cuda.current_stream(device).cuda_stream
-    return c, px, pg, pc
-
-
-def av_scan_workspace(steps, rows, width, gate_per_value=False, backward=False) -> int:
-    """Bytes of workspace av_scan (or av_scan_backward) uses for these sizes."""
-    c = av_scan_config()
-    c.steps, c.rows, c.width, c.gate_per_value = steps, rows, width, int(bool(gate_per_value))
-    n = ctypes.c_size_t(0)
-    _check("av_scan_workspace", load_library().av_scan_workspace(
-        ctypes.byref(c), int(bool(backward)), ctypes.byref(n)))
-    return n.value
-
-
-def _workspace(size_of, name, args, workspace, device):
+def _workspace(size_of, name, config, args, workspace, device):
     """The workspace's tensor (kept alive by the caller), address and size: the caller's, or a
     new one from torch's allocator on the current stream."""
-    torch = _types()[2]
+    torch = _known[2]
     if workspace is None:
         n = ctypes.c_size_t(0)
-        rc = size_of(*args, ctypes.byref(n))
+        rc = size_of(config, *args, ctypes.byref(n))
         if rc:
             _check(name, rc)
         if n.value == 0:
             return None, None, 0
         workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
-    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or \
-            workspace.device != device:
+    elif not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or \
+            not workspace.is_contiguous() or workspace.device != device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
     return workspace, workspace.data_ptr(), workspace.numel()
+
+
+def _scan_common(x, gate, cut, form):
+    """Checks what both passes share: (floating type number, form, strides and address of x and
+    gate, whether the gate is per value, strides and address of cut)."""
+    floats, _, torch, tensor, _, _ = _types()
+    if not isinstance(x, tensor) or not x.is_cuda or x.dim() != 3 or x.dtype not in floats:
+        raise TypeError("x must be a float32, float16 or bfloat16 device tensor [T][B][D]")
+    if not isinstance(gate, tensor):
+        raise TypeError("gate must be a device tensor")
+    shape, device, dtype = x.shape, x.device, x.dtype
+    if shape[1] == 0 or shape[2] == 0:
+        raise ValueError(f"an empty recurrence: x has shape {tuple(shape)}")
+    px, sx = _operand(x, "x", dtype, shape, device)
+    per_value = gate.dim() == 1
+    pg, sg = _operand(gate, "gate", dtype, shape[2:] if per_value else shape, device)
+    pc, sc = None, (0, 0)
+    if cut is not None:
+        _check_tensor(cut, "cut", torch.uint8, shape[:2], device)
+        pc, sc = cut.data_ptr(), cut.stride()
+    return (floats[dtype], SCAN_FORMS[form] if isinstance(form, str) else int(form), px, sx, pg,
+            (0, 0) if per_value else sg, int(per_value), pc, sc)
+
+
+def av_scan_workspace(steps, rows, width, gate_per_value=False, backward=False, dtype=AV_F32) -> int:
+    """Bytes of workspace av_scan (or av_scan_backward) uses for these sizes (dtype: AV_F32, AV_F16
+    or AV_BF16)."""
+    c = av_scan_config()
+    c.steps, c.rows, c.width, c.gate_per_value = steps, rows, width, int(bool(gate_per_value))
+    c.dtype = dtype
+    n = ctypes.c_size_t(0)
+    _check("av_scan_workspace", load_library().av_scan_workspace(
+        ctypes.byref(c), int(bool(backward)), ctypes.byref(n)))
+    return n.value
 
 
 def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=False,
@@ -545,17 +544,17 @@ def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=Fal
     gate the same, or [D]; h0, last: float32 [B][D] or None; cut: uint8 [T][B] or None (a step
     whose flag is set starts anew).  y may be x.  Runs on the current stream of x's device."""
     lib = load_library()
-    c, px, pg, pc = _scan_config(x, gate, cut, form, reverse)
+    kind, form, px, sx, pg, sg, per_value, pc, sc = _scan_common(x, gate, cut, form)
     shape, device = x.shape, x.device
-    py, s = _operand(y, "y", x.dtype, shape, device)
-    c.y_step, c.y_row = s[0], s[1]
-    f32 = _types()[2].float32
+    py, sy = _operand(y, "y", x.dtype, shape, device)
+    f32, stream = _known[4], _known[5]
     ph = _packed(h0, "h0", f32, shape[1:], device)
     pl = _packed(last, "last", f32, shape[1:], device)
-    ref = ctypes.byref(c)
-    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", (ref, 0), workspace,
-                             device)
-    rc = lib.av_scan(ref, px, pg, pc, ph, py, pl, pw, n)
+    c = _SCAN.pack(*shape, kind, form, 1 if reverse else 0, per_value, sx[0], sx[1], sg[0], sg[1],
+                   sy[0], sy[1], sc[0], sc[1], 0, 0, 0, 0, 0, 0, device.index, 0,
+                   stream(device.index))
+    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", c, (0,), workspace, device)
+    rc = lib.av_scan(c, px, pg, pc, ph, py, pl, pw, n)
     if rc:
         _check("av_scan", rc)
 
@@ -565,49 +564,49 @@ def av_scan_backward(x, gate, y, dy, dx, dgate=None, h0=None, dlast=None, dh0=No
     """Gradients of av_scan, called as it was: y its output, dy and dlast the gradients of y and
     last; dx, dgate (like gate, or None) and dh0 (float32 [B][D], or None) are written."""
     lib = load_library()
-    c, px, pg, pc = _scan_config(x, gate, cut, form, reverse)
+    kind, form, px, sx, pg, sg, per_value, pc, sc = _scan_common(x, gate, cut, form)
     shape, device, dtype = x.shape, x.device, x.dtype
-    py, s = _operand(y, "y", dtype, shape, device)
-    c.y_step, c.y_row = s[0], s[1]
-    pdy, s = _operand(dy, "dy", dtype, shape, device)
-    c.dy_step, c.dy_row = s[0], s[1]
-    pdx, s = _operand(dx, "dx", dtype, shape, device)
-    c.dx_step, c.dx_row = s[0], s[1]
-    if c.gate_per_value:
+    py, sy = _operand(y, "y", dtype, shape, device)
+    pdy, sdy = _operand(dy, "dy", dtype, shape, device)
+    pdx, sdx = _operand(dx, "dx", dtype, shape, device)
+    pdg, sdg = None, (0, 0)
+    if per_value:
         pdg = _packed(dgate, "dgate", dtype, shape[2:], device)
-    else:
-        pdg, s = _operand(dgate, "dgate", dtype, shape, device)
-        c.dgate_step, c.dgate_row = s[0], s[1]
-    f32 = _types()[2].float32
+    elif dgate is not None:
+        pdg, sdg = _operand(dgate, "dgate", dtype, shape, device)
+    f32, stream = _known[4], _known[5]
     ph = _packed(h0, "h0", f32, shape[1:], device)
     pdl = _packed(dlast, "dlast", f32, shape[1:], device)
     pdh = _packed(dh0, "dh0", f32, shape[1:], device)
-    ref = ctypes.byref(c)
-    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", (ref, 1), workspace,
-                             device)
-    rc = lib.av_scan_backward(ref, px, pg, pc, ph, py, pdy, pdl, pdx, pdg, pdh, pw, n)
+    c = _SCAN.pack(*shape, kind, form, 1 if reverse else 0, per_value, sx[0], sx[1], sg[0], sg[1],
+                   sy[0], sy[1], sc[0], sc[1], sdy[0], sdy[1], sdx[0], sdx[1], sdg[0], sdg[1],
+                   device.index, 0, stream(device.index))
+    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", c, (1,), workspace, device)
+    rc = lib.av_scan_backward(c, px, pg, pc, ph, py, pdy, pdl, pdx, pdg, pdh, pw, n)
     if rc:
         _check("av_scan_backward", rc)
 
 
-def _tokens_config(logits, ids):
-    floats, whole, torch = _types()
-    if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dim() != 2 or \
+def _logits(logits):
+    """The logits' address, row stride and floating type number."""
+    floats, _, _, tensor, _, _ = _types()
+    if not isinstance(logits, tensor) or not logits.is_cuda or logits.dim() != 2 or \
             logits.dtype not in floats:
         raise TypeError("logits must be a float32, float16 or bfloat16 device tensor [N][A]")
-    shape, device = logits.shape, logits.device
-    pl, s = _operand(logits, "logits", logits.dtype, shape, device)
-    c = av_tokens_config()
-    c.rows, c.choices, c.dtype, c.row_stride = shape[0], shape[1], floats[logits.dtype], s[0]
-    pi = None
-    if ids is not None:
-        if not isinstance(ids, torch.Tensor) or ids.dtype not in whole:
-            raise TypeError("ids must be a uint8, int32 or int64 device tensor [N]")
-        c.ids_type = whole[ids.dtype]
-        pi = _packed(ids, "ids", ids.dtype, shape[:1], device)
-    c.device = device.index
-    c.stream = torch.cuda.current_stream(device).cuda_stream
-    return c, pl, pi
+    strides = logits.stride()
+    if strides[1] != 1 and logits.shape[1] > 1:
+        raise ValueError("the last dimension of logits must be contiguous")
+    return logits.data_ptr(), strides[0], floats[logits.dtype]
+
+
+def _token_ids(ids, rows, device):
+    """The given tokens' address and type number."""
+    if ids is None:
+        return None, 0
+    whole = _known[1]
+    if not isinstance(ids, _known[3]) or ids.dtype not in whole:
+        raise TypeError("ids must be a uint8, int32 or int64 device tensor [N]")
+    return _packed(ids, "ids", ids.dtype, rows, device), whole[ids.dtype]
 
 
 def av_log_probs_workspace(rows, choices, top=0, dtype=AV_F32) -> int:
@@ -626,24 +625,27 @@ def av_log_probs(logits, ids=None, logp=None, entropy=None, stats=None, top_logp
     int64 [N] (outside [0, A): padding); logp, entropy: float32 [N]; stats: float32 [N][2], for
     av_log_probs_backward; top_logp, top_ids: float32 / int32 [N][k], the k <= 32 most likely.
     What is None is not written.  Runs on the current stream of the logits' device."""
-    c, pl, pi = _tokens_config(logits, ids)
-    torch, device, N = _types()[2], logits.device, logits.shape[0]
-    f32 = torch.float32
-    row = logits.shape[:1]
-    p = [_packed(logp, "logp", f32, row, device), _packed(entropy, "entropy", f32, row, device),
-         _packed(stats, "stats", f32, (N, 2), device)]
+    lib = load_library()
+    pl, stride, kind = _logits(logits)
+    _, _, torch, _, f32, stream = _known
+    shape, device = logits.shape, logits.device
+    N, row = shape[0], shape[:1]
+    pi, ids_type = _token_ids(ids, row, device)
+    plp = _packed(logp, "logp", f32, row, device)
+    pe = _packed(entropy, "entropy", f32, row, device)
+    ps = _packed(stats, "stats", f32, (N, 2), device)
+    top, ptl, pti = 0, None, None
     if top_logp is not None or top_ids is not None:
         if top_logp is None or top_ids is None or top_logp.dim() != 2:
             raise ValueError("top_logp and top_ids [N][k] go together")
-        c.top = top_logp.shape[1]
-        p += [_packed(top_logp, "top_logp", f32, (N, c.top), device),
-              _packed(top_ids, "top_ids", torch.int32, (N, c.top), device)]
-    else:
-        p += [None, None]
-    lib, ref = load_library(), ctypes.byref(c)
-    keep, pw, n = _workspace(lib.av_log_probs_workspace, "av_log_probs_workspace", (ref,),
-                             workspace, device)
-    rc = lib.av_log_probs(ref, pl, pi, *p, pw, n)
+        top = top_logp.shape[1]
+        ptl = _packed(top_logp, "top_logp", f32, (N, top), device)
+        pti = _packed(top_ids, "top_ids", torch.int32, (N, top), device)
+    c = _TOKENS.pack(N, shape[1], kind, ids_type, stride, 0, top, device.index,
+                     stream(device.index))
+    keep, pw, n = _workspace(lib.av_log_probs_workspace, "av_log_probs_workspace", c, (), workspace,
+                             device)
+    rc = lib.av_log_probs(c, pl, pi, plp, pe, ps, ptl, pti, pw, n)
     if rc:
         _check("av_log_probs", rc)
 
@@ -651,12 +653,17 @@ def av_log_probs(logits, ids=None, logp=None, entropy=None, stats=None, top_logp
 def av_log_probs_backward(logits, ids, stats, entropy, dlogp, dentropy, dlogits):
     """Gradient of av_log_probs: stats and entropy as it stored them, dlogp and dentropy float32
     [N] or None (then ids, or entropy, may be None too), dlogits like logits; it may be logits."""
-    c, pl, pi = _tokens_config(logits, ids)
-    f32, device, row = _types()[2].float32, logits.device, logits.shape[:1]
-    pd, s = _operand(dlogits, "dlogits", logits.dtype, logits.shape, device)
-    c.drow_stride = s[0]
-    rc = load_library().av_log_probs_backward(
-        ctypes.byref(c), pl, pi, _packed(stats, "stats", f32, (row[0], 2), device),
+    lib = load_library()
+    pl, stride, kind = _logits(logits)
+    f32, stream = _known[4], _known[5]
+    shape, device = logits.shape, logits.device
+    row = shape[:1]
+    pi, ids_type = _token_ids(ids, row, device)
+    pd, sd = _operand(dlogits, "dlogits", logits.dtype, shape, device)
+    c = _TOKENS.pack(shape[0], shape[1], kind, ids_type, stride, sd[0], 0, device.index,
+                     stream(device.index))
+    rc = lib.av_log_probs_backward(
+        c, pl, pi, _packed(stats, "stats", f32, (row[0], 2), device),
         _packed(entropy, "entropy", f32, row, device), _packed(dlogp, "dlogp", f32, row, device),
         _packed(dentropy, "dentropy", f32, row, device), pd)
     if rc:
@@ -666,12 +673,17 @@ def av_log_probs_backward(logits, ids, stats, entropy, dlogp, dentropy, dlogits)
 def av_draw_actions(logits, uniform, actions, logp=None):
     """Draw an action per row of logits [N][A], A <= 256: uniform float32 [N] in [0, 1), actions
     uint8 [N], logp float32 [N] or None."""
-    c, pl, _ = _tokens_config(logits, None)
-    torch, device, row = _types()[2], logits.device, logits.shape[:1]
-    rc = load_library().av_draw_actions(
-        ctypes.byref(c), pl, _packed(uniform, "uniform", torch.float32, row, device),
-        _packed(actions, "actions", torch.uint8, row, device),
-        _packed(logp, "logp", torch.float32, row, device))
+    lib = load_library()
+    pl, stride, kind = _logits(logits)
+    _, _, torch, _, f32, raw_stream = _known
+    shape, device = logits.shape, logits.device
+    row = shape[:1]
+    pu = _packed(uniform, "uniform", f32, row, device)
+    pa = _packed(actions, "actions", torch.uint8, row, device)
+    plp = _packed(logp, "logp", f32, row, device)
+    c = _TOKENS.pack(shape[0], shape[1], kind, 0, stride, 0, 0, device.index,
+                     raw_stream(device.index))
+    rc = lib.av_draw_actions(c, pl, pu, pa, plp)
     if rc:
         _check("av_draw_actions", rc)
 

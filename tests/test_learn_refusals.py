@@ -168,3 +168,12 @@ def test_binding_refuses_host_tensors():
         av.av_log_probs(torch.zeros((2, 3)))
     with pytest.raises(TypeError):
         av.av_draw_actions(torch.zeros((2, 3)), torch.zeros(2), torch.zeros(2, dtype=torch.uint8))
+
+
+def test_packed_configs_have_the_structs_layout():
+    """The binding packs its configs in one step: field for field what the structs hold."""
+    for pack, struct in ((av._SCAN, av.av_scan_config), (av._TOKENS, av.av_tokens_config)):
+        assert pack.size == ctypes.sizeof(struct)
+        values = list(range(1, len(struct._fields_) + 1))
+        c = struct.from_buffer_copy(pack.pack(*values))
+        assert [getattr(c, f) for f, _ in struct._fields_] == values
