@@ -583,10 +583,13 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 // not all be aligned; far: rows too far apart for a wave's addressing.
 //   A few steps, or far rows: a lane takes its columns through all of them.
 //   Else a lane takes a word of columns where that still fills the device, for its longer row
-//   segments (128 x 1024 x 256 in bf16: 42 us forward, 54 with single columns), and one column
-//   where it would not (2048 x 64 x 256: 62 us, with words 151); as many waves as the steps have use
-//   for; and chunks of time where single columns leave compute units idle and the steps are at least
-//   eight tiles (below that the second launch costs more than the idle units).
+//   segments (128 x 1024 x 256 in bf16: 42 us forward, with single columns 50), and one column
+//   where only that does (2048 x 64 x 256: 58 us, with words 151).  Where neither does, time is cut
+//   into chunks, if there are more than three tiles of eight waves (below that the second launch
+//   costs more than the idle units), and words are taken again.
+//   Waves: eight, or sixteen where there is at most one uncut workgroup a compute unit, which has to
+//   hide its own latency (1000 x 16384 in f32: 26.3 us, with eight 27.7; but 300 x 500 x 33, some
+//   units with two workgroups: 22.1 with sixteen, 18.4 with eight).
 ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int wide, bool far, bool col, bool back) {
     ScanPlan plan{};
     const int64_t N = B * D;
@@ -597,10 +600,12 @@ ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int wide, bool far, bool col
         // words where they fill the device, or where chunks of time will have to anyway
         if (N / wide < int64_t(64) * kFill && N >= int64_t(64) * kFill / 2) plan.vec = 1;
         const int64_t K = steps_of(plan.vec), groups = scan_groups(N, plan.vec);
-        plan.waves = int(std::min<int64_t>(waves_of(plan.vec), (T + K - 1) / K));
-        const int64_t tile = plan.waves * K, tiles = (T + tile - 1) / tile;
-        const int64_t want = std::min((kFill + groups - 1) / groups, tiles);
-        if (tiles >= 4 && groups < kFill / 2) {
+        const bool cut = groups < kFill / 2 && T > 3 * 8 * K;
+        plan.waves = int(std::min<int64_t>(cut || groups > kFill / 2 ? 8 : waves_of(plan.vec),
+                                           (T + K - 1) / K));
+        if (cut) {
+            const int64_t tile = plan.waves * K, tiles = (T + tile - 1) / tile;
+            const int64_t want = std::min((kFill + groups - 1) / groups, tiles);
             plan.chunk = (tiles + want - 1) / want * tile;
             plan.chunks = int((T + plan.chunk - 1) / plan.chunk);
         }

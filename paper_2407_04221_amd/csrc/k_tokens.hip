@@ -129,17 +129,23 @@ __device__ inline void put_top(const TokenArgs &a, const Row &r, int64_t row, in
     a.top_logp[row * a.top + j] = r.bad ? __builtin_nanf("") : none ? kNone : logp_of(r, key_logit(k));
 }
 
-template <typename T>
-__device__ inline void put_row(const TokenArgs &a, const Row &r, int64_t row, const T *l) {
+// The given token's logit, fetched before the row is worked on; inside: it is one of the choices.
+struct Given { bool inside; float l; };
+
+template <typename T> __device__ inline Given given_of(const TokenArgs &a, int64_t row, const T *l) {
+    Given g{false, kNone};
     if (a.logp) {
         const int64_t id = id_of(a, row);
-        float v = 0.0f;
-        if (id >= 0 && id < a.A) {
-            const float x = to_f32(l[id]);
-            v = r.bad ? __builtin_nanf("") : x == kNone ? kNone : logp_of(r, x);
-        }
-        a.logp[row] = v;
+        g.inside = id >= 0 && id < a.A;
+        if (g.inside) g.l = to_f32(l[id]);
     }
+    return g;
+}
+
+__device__ inline void put_row(const TokenArgs &a, const Row &r, int64_t row, const Given &g) {
+    if (a.logp)
+        a.logp[row] = !g.inside ? 0.0f : r.bad ? __builtin_nanf("") : g.l == kNone ? kNone
+                                                                          : logp_of(r, g.l);
     if (a.entropy) a.entropy[row] = r.entropy;
     if (a.stats) {
         a.stats[2 * row] = r.m;
@@ -154,11 +160,36 @@ template <typename T, int kA> __device__ inline void load_small(const T *l, int 
     for (int i = 0; i < kA; ++i) v[i] = i < A ? to_f32(l[i]) : kNone;
 }
 
-template <typename T, int kA>
+// The rows of a workgroup, which lie one behind the other, between memory and LDS as 16-byte
+// words (and what is left over at the end of the last workgroup's rows element by element).
+template <typename T, bool kIn> __device__ inline void move_rows(T *tile, T *rows, int elements) {
+    typedef uint32_t Word __attribute__((ext_vector_type(4)));
+    constexpr int kPer = 16 / sizeof(T);
+    const int words = elements / kPer;
+    for (int w = threadIdx.x; w < words; w += 256) {
+        if (kIn) reinterpret_cast<Word *>(tile)[w] = reinterpret_cast<const Word *>(rows)[w];
+        else __builtin_nontemporal_store(reinterpret_cast<Word *>(tile)[w],
+                                         reinterpret_cast<Word *>(rows) + w);
+    }
+    for (int i = words * kPer + threadIdx.x; i < elements; i += 256) {
+        if (kIn) tile[i] = rows[i];
+        else rows[i] = tile[i];
+    }
+}
+
+template <typename T, int kA, bool kTile>
 __global__ void __launch_bounds__(256) small_rows_kernel(TokenArgs a) {
-    const int64_t row = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (row >= a.N) return;
+    __shared__ __attribute__((aligned(16))) T tile[kTile ? 256 * kA : 1];
+    const int64_t row0 = int64_t(blockIdx.x) * 256, row = row0 + threadIdx.x;
     const T *l = static_cast<const T *>(a.logits) + row * a.stride;
+    if (kTile) {
+        const T *rows = static_cast<const T *>(a.logits) + row0 * a.stride;
+        move_rows<T, true>(tile, const_cast<T *>(rows), int(min(int64_t(256), a.N - row0)) * a.A);
+        __syncthreads();
+        l = tile + threadIdx.x * a.A;
+    }
+    if (row >= a.N) return;
+    const Given given = given_of(a, row, l);
     float v[kA];
     load_small(l, a.A, v);
     Stat st{kNone, 0.0f, 0.0f};
@@ -167,7 +198,7 @@ __global__ void __launch_bounds__(256) small_rows_kernel(TokenArgs a) {
 #pragma unroll
     for (int i = 0; i < kA; ++i) add(st, v[i]);
     const Row r = row_of(st);
-    put_row(a, r, row, l);
+    put_row(a, r, row, given);
     if (a.top) {
         uint64_t last = ~uint64_t(0);
         for (int j = 0; j < a.top; ++j) {
@@ -219,19 +250,32 @@ template <int n> __device__ inline void slopes(const Back &b, int at, float (&v)
     }
 }
 
-template <typename T, int kA>
+template <typename T, int kA, bool kTile>
 __global__ void __launch_bounds__(256) small_back_kernel(TokenArgs a) {
-    const int64_t row = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (row >= a.N) return;
+    __shared__ __attribute__((aligned(16))) T tile[kTile ? 256 * kA : 1];
+    const int64_t row0 = int64_t(blockIdx.x) * 256, row = row0 + threadIdx.x;
+    const int rows = int(min(int64_t(256), a.N - row0));
     const T *l = static_cast<const T *>(a.logits) + row * a.stride;
     T *d = static_cast<T *>(a.dlogits) + row * a.dstride;
-    const Back b = back_of(a, row);
-    float v[kA];
-    load_small(l, a.A, v);
-    slopes(b, 0, v);
+    if (kTile) {
+        const T *from = static_cast<const T *>(a.logits) + row0 * a.stride;
+        move_rows<T, true>(tile, const_cast<T *>(from), rows * a.A);
+        __syncthreads();
+        l = d = tile + threadIdx.x * a.A;
+    }
+    if (row < a.N) {
+        const Back b = back_of(a, row);
+        float v[kA];
+        load_small(l, a.A, v);
+        slopes(b, 0, v);
 #pragma unroll
-    for (int i = 0; i < kA; ++i)
-        if (i < a.A) d[i] = from_f32<T>(v[i]);
+        for (int i = 0; i < kA; ++i)
+            if (i < a.A) d[i] = from_f32<T>(v[i]);
+    }
+    if (kTile) {
+        __syncthreads();
+        move_rows<T, false>(tile, static_cast<T *>(a.dlogits) + row0 * a.dstride, rows * a.A);
+    }
 }
 
 // ---- longer rows, as aligned words of kPer elements ----
@@ -315,6 +359,8 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= a.N) return;
     const Words<T> in(a, row);
+    Given given{};
+    if (lane == 0) given = given_of(a, row, in.l);
     float v[kWords][kPer];
 #pragma unroll
     for (int j = 0; j < kWords; ++j) in.load(j * 64 + lane, v[j]);
@@ -329,7 +375,7 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     st.s = wave_sum(st.s);
     st.w = wave_sum(st.w);
     const Row r = row_of(st);
-    if (lane == 0) put_row(a, r, row, in.l);
+    if (lane == 0) put_row(a, r, row, given);
     if (a.top == 0) return;
     unsigned long long *list = lists[threadIdx.x >> 6];
     const uint64_t bound = uint64_t(kth_of_wave(uint32_t(key_of(m, 0) >> 32), a.top)) << 32;
@@ -531,6 +577,8 @@ __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t row = blockIdx.x;
     const Parts<T> in(a, row, kSplit ? blockIdx.y : 0, kSplit ? a.parts : 1);
+    Given given{};
+    if (!kSplit && tid == 0) given = given_of(a, row, in.l);
     // the row's ends
     const int before = in.single(tid, false), after = in.single(tid, true);
     const float va = before >= 0 ? to_f32(in.l[before]) : kNone;
@@ -576,7 +624,7 @@ __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
         return;
     }
     const Row r = row_of(all);
-    if (tid == 0) put_row(a, r, row, in.l);
+    if (tid == 0) put_row(a, r, row, given);
     if (a.top)
         alternatives<T, kThreads>(a, in, mine, [&](int place, uint64_t k) {
             put_top(a, r, row, place, k);
@@ -589,32 +637,34 @@ template <typename T> __global__ void __launch_bounds__(256) join_rows_kernel(To
     __shared__ uint64_t keys[64 * AV_TOP_MAX];
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
+    Given given{};
+    if (tid == 0)
+        given = given_of(a, row, static_cast<const T *>(a.logits) + row * a.stride);
+    const int n = a.parts * a.top;
+    for (int i = tid; i < n; i += 256) keys[i] = a.part_keys[row * n + i];
     Stat all{kNone, 0.0f, 0.0f};
     if (lane < a.parts) all = static_cast<const Stat *>(a.part_stats)[row * a.parts + lane];
     const Row r = row_of(join_lanes(all));
-    if (tid == 0) put_row(a, r, row, static_cast<const T *>(a.logits) + row * a.stride);
+    if (tid == 0) put_row(a, r, row, given);
     if (a.top == 0) return;
-    const int n = a.parts * a.top;
-    for (int i = tid; i < n; i += 256) keys[i] = a.part_keys[row * n + i];
     __syncthreads();
-    // larger keys than k in a part's falling list
+    // how many keys of a part's falling list are larger than k
     auto larger = [&](int part, uint64_t k) {
-        int lo = 0, hi = a.top;
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (keys[part * a.top + mid] > k) lo = mid + 1;
-            else hi = mid;
-        }
-        return lo;
+        const uint64_t *list = keys + part * a.top;
+        int at = 0;
+#pragma unroll
+        for (int step = AV_TOP_MAX; step > 0; step /= 2)
+            if (at + step <= a.top && list[at + step - 1] > k) at += step;
+        return at;
     };
     for (int i = tid; i < n; i += 256) {
         if (keys[i] == 0) continue;
         int place = 0;
+#pragma unroll 4
         for (int p = 0; p < a.parts; ++p) place += larger(p, keys[i]);
         if (place < a.top) put_top(a, r, row, place, keys[i]);
     }
-    int live = 0;
-    for (int p = 0; p < a.parts; ++p) live += larger(p, 0);
+    const int live = int(wave_sum(lane < a.parts ? float(larger(lane, 0)) : 0.0f));
     for (int j = live + tid; j < a.top; j += 256) put_top(a, r, row, j, 0);
 }
 
@@ -748,14 +798,32 @@ template <typename T> int words_of(const TokenArgs &a) {     // most words a row
     return int((int64_t(a.A) + 16 / sizeof(T) - 2) / (16 / sizeof(T))) + 1;
 }
 
+// Rows one behind the other from a 16-byte border on: moved through LDS.
+bool packed_rows(const TokenArgs &a, const void *p, int64_t stride) {
+    return (stride == a.A || a.N == 1) && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+}
+
+template <typename T, bool kTile> hipError_t small_forward(const TokenArgs &a, hipStream_t s) {
+    const dim3 g(blocks_of(a.N, 256)), b(256);
+    if (a.A <= 4) hipLaunchKernelGGL((small_rows_kernel<T, 4, kTile>), g, b, 0, s, a);
+    else if (a.A <= 8) hipLaunchKernelGGL((small_rows_kernel<T, 8, kTile>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((small_rows_kernel<T, 16, kTile>), g, b, 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T, bool kTile> hipError_t small_backward(const TokenArgs &a, hipStream_t s) {
+    const dim3 g(blocks_of(a.N, 256)), b(256);
+    if (a.A <= 4) hipLaunchKernelGGL((small_back_kernel<T, 4, kTile>), g, b, 0, s, a);
+    else if (a.A <= 8) hipLaunchKernelGGL((small_back_kernel<T, 8, kTile>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((small_back_kernel<T, 16, kTile>), g, b, 0, s, a);
+    return hipGetLastError();
+}
+
 template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
     const dim3 b(256);
     if (a.A <= kThreadRow) {
-        const dim3 g(blocks_of(a.N, 256));
-        if (a.A <= 4) hipLaunchKernelGGL((small_rows_kernel<T, 4>), g, b, 0, s, a);
-        else if (a.A <= 8) hipLaunchKernelGGL((small_rows_kernel<T, 8>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((small_rows_kernel<T, 16>), g, b, 0, s, a);
-        return hipGetLastError();
+        if (packed_rows(a, a.logits, a.stride)) return small_forward<T, true>(a, s);
+        return small_forward<T, false>(a, s);
     }
     const int lanes = blocks_of(words_of<T>(a), 64);
     if (a.A <= kWaveRow && lanes <= 8) {
@@ -783,11 +851,9 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
 template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
     const dim3 b(256);
     if (a.A <= kThreadRow) {
-        const dim3 g(blocks_of(a.N, 256));
-        if (a.A <= 4) hipLaunchKernelGGL((small_back_kernel<T, 4>), g, b, 0, s, a);
-        else if (a.A <= 8) hipLaunchKernelGGL((small_back_kernel<T, 8>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((small_back_kernel<T, 16>), g, b, 0, s, a);
-        return hipGetLastError();
+        if (packed_rows(a, a.logits, a.stride) && packed_rows(a, a.dlogits, a.dstride))
+            return small_backward<T, true>(a, s);
+        return small_backward<T, false>(a, s);
     }
     constexpr int kPer = 16 / sizeof(T);
     const bool same = (reinterpret_cast<uintptr_t>(a.logits) -
