@@ -169,6 +169,56 @@ def bench_mutation(av, torch, wl, maps, rules, stream, seed):
                       "us_per_call": us_rules, "roofline": roof(rule_bytes, us_rules)}}
 
 
+def bench_learn(av, torch, wl, b, acts, stream, width, seed):
+    """The learner's side of a rollout of up to 100 steps of the workload: an action drawn for every
+    environment, the discounted returns of the rollout's rewards and done flags, an agent's memory of
+    `width` values an environment over it (bf16, forward and gradient, starting anew after every
+    episode), and the log-probabilities of its actions with their gradient.  Bytes: each input read
+    once, each output written once."""
+    k = min(acts.shape[0], 100)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rewards, done = b.step_n(acts[:k])
+    n, D = k * wl.B, width
+
+    def roof(nbytes, us):
+        gbs = nbytes / (us * 1e-6) / 1e9
+        return {"us_per_call": us,
+                "roofline": {"bound": "hbm", "achieved": gbs, "peak": HBM_PEAK_GBS, "unit": "GB/s",
+                             "frac": gbs / HBM_PEAK_GBS, "bytes_per_call": int(nbytes)}}
+
+    def normal(*shape, dtype=torch.float32):
+        return torch.randn(shape, generator=g, device="cuda").to(dtype)
+    logits, uniform = normal(wl.B, 5), torch.rand(wl.B, generator=g, device="cuda")
+    drawn = torch.empty(wl.B, dtype=torch.uint8, device="cuda")
+    drawn_logp = torch.empty(wl.B, device="cuda")
+    out = {"steps": k, "width": D}
+    us = _time_us(lambda: b.act(logits, uniform, drawn, drawn_logp), stream, torch)
+    out["act"] = {"api": "av_draw_actions", **roof(wl.B * (5 * 4 + 4 + 1 + 4), us)}
+    gamma, returns = torch.full((1,), 0.99, device="cuda"), torch.empty_like(rewards)
+    us = _time_us(lambda: b.returns(rewards, done, gamma, out=returns), stream, torch)
+    out["returns"] = {"api": "av_scan", **roof(n * 9, us)}
+    flags = torch.cat((torch.zeros_like(done[:1]), done[:-1]))      # done before the step
+    bf16 = torch.bfloat16
+    x, gate, dy = (normal(k, wl.B, D, dtype=bf16) for _ in range(3))
+    y, dx, dgate = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    us = _time_us(lambda: av.av_scan(x, gate, y, cut=flags, form="gated"), stream, torch, reps=20)
+    out["memory"] = {"api": "av_scan", **roof(n * (3 * D * 2 + 1), us)}
+    us = _time_us(lambda: av.av_scan_backward(x, gate, y, dy, dx, dgate, cut=flags, form="gated"),
+                  stream, torch, reps=20)
+    out["memory_gradient"] = {"api": "av_scan_backward", **roof(n * (6 * D * 2 + 1), us)}
+    del x, gate, dy, y, dx, dgate
+    logits, ids = normal(n, 5), acts[:k].reshape(n)
+    logp, entropy = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    stats, dlogits = torch.empty((n, 2), device="cuda"), torch.empty_like(logits)
+    us = _time_us(lambda: av.av_log_probs(logits, ids, logp, entropy, stats), stream, torch)
+    out["log_probs"] = {"api": "av_log_probs", **roof(n * (5 * 4 + 1 + 16), us)}
+    dlogp, dentropy = -returns.reshape(n) / n, torch.full((n,), -0.01 / n, device="cuda")
+    us = _time_us(lambda: av.av_log_probs_backward(logits, ids, stats, entropy, dlogp, dentropy,
+                                                   dlogits), stream, torch)
+    out["log_probs_gradient"] = {"api": "av_log_probs_backward", **roof(n * (10 * 4 + 1 + 20), us)}
+    return out
+
+
 def bench_search(av, torch, wl, args):
     """av_search_* from environment 0's map and rule set: levels until the frontier empties or
     the budget of visits is spent.  Timed with the host clock around the whole search (each
@@ -306,6 +356,9 @@ def main():
                     help="also time av_observe with a W x W window (HBM-bound gather)")
     ap.add_argument("--mutate", action="store_true",
                     help="also time the mutation operators on the workload's population")
+    ap.add_argument("--learn", type=int, default=0, metavar="D",
+                    help="also time the learner's operators on a rollout of the workload, with an "
+                         "agent's memory of D values per environment")
     ap.add_argument("--search", type=int, default=0, metavar="BUDGET",
                     help="also time the batched search from environment 0 with this many visits")
     ap.add_argument("--search-variant", default="dense", choices=["literal", "planted", "dense"])
@@ -456,6 +509,10 @@ def main():
     if args.mutate:
         mutate = bench_mutation(av, torch, wl, maps, rules, stream, args.seed)
 
+    learn = None
+    if args.learn:
+        learn = bench_learn(av, torch, wl, b, acts, stream, args.learn, args.seed)
+
     cpu = None
     if not args.no_cpu:
         cpu = cpu_baseline(wl, maps, rules, actions, args.cpu_seconds,
@@ -521,6 +578,7 @@ def main():
         "per_launch_path": per_launch,
         "observe": observe,
         "mutate": mutate,
+        "learn": learn,
         "search": search,
         "cpu_baseline": cpu,
     }

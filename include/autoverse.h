@@ -443,8 +443,8 @@ typedef enum {
  * the width is contiguous).  Strides are not negative; inputs may have strides of 0 (a broadcast
  * input). */
 typedef struct {
-    int64_t steps;            /* T in [0, 2^31) */
-    int64_t rows, width;      /* B >= 0, D >= 1, B x D < 2^31 */
+    int64_t steps;            /* T in [0, 2^30] */
+    int64_t rows, width;      /* B >= 0, D >= 1, B x D <= 2^28 */
     int32_t dtype;            /* av_dtype of x, gate, y and their gradients */
     int32_t form;             /* av_scan_form */
     int32_t reverse;          /* 0: t runs 0 .. T-1; 1: T-1 .. 0 ("t - 1" below is then t + 1) */

@@ -55,14 +55,18 @@ av_status launched(const char *what, hipError_t e) {
 
 size_t size_of(int dtype) { return dtype == AV_F32 ? 4 : 2; }
 
-constexpr int64_t kBig = int64_t(1) << 31;
+constexpr int64_t kBig = int64_t(1) << 31, kMostSteps = int64_t(1) << 30;
+constexpr int64_t kMostColumns = int64_t(1) << 28;
 
 av_status check_scan(const av_scan_config *c) {
     if (!c) return bad("cfg is NULL");
-    if (c->steps < 0 || c->steps >= kBig) return bad("steps %lld outside [0, 2^31)", (long long)c->steps);
-    if (c->rows < 0 || c->width < 1 || c->rows >= kBig || c->width >= kBig ||
-        c->rows * c->width >= kBig)
-        return bad("rows %lld, width %lld: needs rows >= 0, width >= 1, rows x width < 2^31",
+    // steps are counted in 32 bits a tile past the end; a launch has fewer than 2^32 threads, up to
+    // eight a column; and a lane's distance within a row, in bytes, fits 32 bits
+    if (c->steps < 0 || c->steps > kMostSteps)
+        return bad("steps %lld outside [0, 2^30]", (long long)c->steps);
+    if (c->rows < 0 || c->width < 1 || c->rows > kMostColumns || c->width > kMostColumns ||
+        c->rows * c->width > kMostColumns)
+        return bad("rows %lld, width %lld: needs rows >= 0, width >= 1, rows x width <= 2^28",
                    (long long)c->rows, (long long)c->width);
     if (c->dtype != AV_F32 && c->dtype != AV_F16 && c->dtype != AV_BF16)
         return bad("unknown dtype %d", c->dtype);

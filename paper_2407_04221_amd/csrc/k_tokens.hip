@@ -899,28 +899,64 @@ TokenPlan tokens_plan(int64_t N, int64_t A, int top, int dtype) {
     return plan;
 }
 
-hipError_t launch_log_probs(const TokenArgs &a, int dtype, hipStream_t s) {
-    switch (dtype) {
-        case AV_F32: return forward<float>(a, s);
-        case AV_F16: return forward<_Float16>(a, s);
-        default: return forward<bf16_t>(a, s);
+// Calls f for runs of at most 2^22 rows: a launch has fewer than 2^32 threads, at most 512 a row
+// where the rows are many.
+template <typename F> static hipError_t in_runs(const TokenArgs &all, int dtype, F f) {
+    constexpr int64_t kRun = int64_t(1) << 22;
+    const int64_t size = dtype == AV_F32 ? 4 : 2;
+    const int64_t id = all.ids_type == AV_IDS_U8 ? 1 : all.ids_type == AV_IDS_I32 ? 4 : 8;
+    for (int64_t row = 0; row < all.N; row += kRun) {
+        TokenArgs a = all;
+        a.N = std::min(kRun, all.N - row);
+        a.logits = static_cast<const char *>(all.logits) + row * all.stride * size;
+        if (all.ids) a.ids = static_cast<const char *>(all.ids) + row * id;
+        if (all.logp) a.logp += row;
+        if (all.entropy) a.entropy += row;
+        if (all.stats) a.stats += 2 * row;
+        if (all.top_logp) a.top_logp += row * all.top;
+        if (all.top_ids) a.top_ids += row * all.top;
+        if (all.in_stats) a.in_stats += 2 * row;
+        if (all.in_entropy) a.in_entropy += row;
+        if (all.dlogp) a.dlogp += row;
+        if (all.dentropy) a.dentropy += row;
+        if (all.dlogits)
+            a.dlogits = static_cast<char *>(all.dlogits) + row * all.dstride * size;
+        if (all.uniform) a.uniform += row;
+        if (all.actions) a.actions += row;
+        const hipError_t e = f(a);
+        if (e != hipSuccess) return e;
     }
+    return hipSuccess;
 }
 
-hipError_t launch_log_probs_backward(const TokenArgs &a, int dtype, hipStream_t s) {
-    switch (dtype) {
-        case AV_F32: return backward<float>(a, s);
-        case AV_F16: return backward<_Float16>(a, s);
-        default: return backward<bf16_t>(a, s);
-    }
+hipError_t launch_log_probs(const TokenArgs &all, int dtype, hipStream_t s) {
+    return in_runs(all, dtype, [&](const TokenArgs &a) {
+        switch (dtype) {
+            case AV_F32: return forward<float>(a, s);
+            case AV_F16: return forward<_Float16>(a, s);
+            default: return forward<bf16_t>(a, s);
+        }
+    });
 }
 
-hipError_t launch_draw(const TokenArgs &a, int dtype, hipStream_t s) {
-    switch (dtype) {
-        case AV_F32: return draw<float>(a, s);
-        case AV_F16: return draw<_Float16>(a, s);
-        default: return draw<bf16_t>(a, s);
-    }
+hipError_t launch_log_probs_backward(const TokenArgs &all, int dtype, hipStream_t s) {
+    return in_runs(all, dtype, [&](const TokenArgs &a) {
+        switch (dtype) {
+            case AV_F32: return backward<float>(a, s);
+            case AV_F16: return backward<_Float16>(a, s);
+            default: return backward<bf16_t>(a, s);
+        }
+    });
+}
+
+hipError_t launch_draw(const TokenArgs &all, int dtype, hipStream_t s) {
+    return in_runs(all, dtype, [&](const TokenArgs &a) {
+        switch (dtype) {
+            case AV_F32: return draw<float>(a, s);
+            case AV_F16: return draw<_Float16>(a, s);
+            default: return draw<bf16_t>(a, s);
+        }
+    });
 }
 
 }  // namespace av

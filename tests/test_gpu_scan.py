@@ -100,6 +100,27 @@ def test_long_few_columns(dtype, form, columns, reverse):
     run(2048, 2, 65, dtype=dtype, form=form, columns=columns, reverse=reverse, cut=None)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("form", ["linear", "gated"])
+@pytest.mark.parametrize("columns", [False, True])
+def test_words_of_columns(dtype, form, columns):
+    """A lane takes an 8-byte word of columns: in chunks of time, for many columns, for few steps."""
+    kw = dict(dtype=dtype, form=form, columns=columns)
+    run(1000, 2, 12, **kw)
+    run(333, 3, 100, reverse=True, cut=None, **kw)
+    run(37, 1100, 128, seed=1, **kw)                 # fills the device; the last tile is not whole
+    run(70, 258, 512, reverse=True, state=False, **kw)
+    for T in (1, 3, 7):
+        run(T, 50, 24, reverse=T == 3, **kw)
+
+
+@pytest.mark.parametrize("columns", [False, True])
+def test_single_columns_that_fill_the_device(columns):
+    """One uncut workgroup of sixteen waves a compute unit, several tiles; then more workgroups."""
+    run(300, 16384, 1, columns=columns, reverse=True, cut=0.02)
+    run(140, 600, 33, columns=columns, form="gated", dtype="bf16")
+
+
 @pytest.mark.parametrize("pad,shift", [(0, 0), (2, 0), (1, 0), (0, 1), (8, 8), (3, 5)])
 @pytest.mark.parametrize("layout", ["time", "batch"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -262,6 +283,35 @@ def test_binding_refuses():
     long = torch.zeros((5000, 1, 4), device="cuda")
     with pytest.raises(av.AvError):
         av.av_scan(long, long, long, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 bytes of elements; and rows further apart than a wave's 32-bit distances."""
+    T, D = 70000, 32768
+    x = torch.randint(-100, 100, (T, 1, D), dtype=torch.int8, device="cuda").half()
+    y, gate = torch.empty_like(x), torch.zeros(D, dtype=torch.float16, device="cuda")
+    av.av_scan(x, gate, y)
+    assert torch.equal(x, y)
+    y.zero_()
+    gate = gate.expand(T, 1, D)
+    av.av_scan(x, gate, y, reverse=True)
+    assert torch.equal(x, y)
+    del x, y
+    apart = (1 << 30) + 16
+    flat = torch.empty(2 * apart + 64, device="cuda")
+    for T, D in ((30, 1), (3, 4)):
+        x = flat.as_strided((T, 3, D), (D, apart, 1))
+        x.copy_(torch.randint(-5, 6, (T, 3, D), device="cuda"))
+        y = torch.empty((T, 3, D), device="cuda")
+        last, dg = torch.empty((3, D), device="cuda"), torch.empty(D, device="cuda")
+        one = torch.ones(D, device="cuda")
+        av.av_scan(x, one, y, last=last)
+        assert torch.equal(y, torch.cumsum(x.contiguous(), 0)) and torch.equal(last, y[-1])
+        dx = torch.empty_like(y)
+        av.av_scan_backward(x, one, y, x, dx, dg)
+        back = torch.flip(torch.cumsum(torch.flip(x.contiguous(), (0,)), 0), (0,))
+        assert torch.equal(dx, back)
+        assert torch.equal(dg, (back[1:] * y[:-1]).sum((0, 1)))
 
 
 def test_streams_graphs_and_workspaces():

@@ -156,6 +156,62 @@ def test_alternatives_of_hard_orders(A, order):
                 compare(logits, np.zeros(N, np.int64), dtype, top=top)
 
 
+@pytest.mark.parametrize("case", ["few_threads", "one_lane_in_three", "equal"])
+def test_alternatives_that_do_not_fit_the_list(case):
+    """The largest values in the hands of fewer than `top` threads, thousands of them; almost all
+    masked; all equal.  One row for all (a stride of 0), so many rows cost no memory."""
+    A, top = 60000, 32
+    i = torch.arange(A)
+    word = i // 4
+    r = np.random.default_rng(7)
+    v = torch.from_numpy(r.normal(size=A)).float()
+    if case == "few_threads":
+        v += torch.where(word % 512 < 31, 100.0, 0.0)
+    elif case == "one_lane_in_three":
+        v = torch.where(word % 64 % 3 == 0, v, -np.inf)
+    else:
+        v = torch.zeros(A)
+    row = torch.empty(A, device="cuda")
+    row.copy_(v)
+    want = ref.tokens(host(row)[None], np.zeros(1, np.int64), top=top)
+    for N in (2, 520, 2100):
+        tl = torch.empty((N, top), device="cuda")
+        ti = torch.empty((N, top), dtype=torch.int32, device="cuda")
+        av.av_log_probs(row.expand(N, A), top_logp=tl, top_ids=ti)
+        for n in (0, N // 2, N - 1):
+            assert np.array_equal(ti[n:n + 1].cpu().numpy(), want["top_ids"])
+            ref.check(host(tl[n:n + 1]), want["top_logp"], f"top_logp, {N} rows")
+
+
+def test_many_rows_and_offsets_past_32_bits():
+    """Rows of more than one launch, and more than 2^32 bytes of logits: the last rows come out as
+    they do alone."""
+    for N, A, dtype in (((1 << 22) + 5, 17, "f16"), (70001, 32768, "f16"), ((1 << 22) + 3, 4, "f32"),
+                        ((1 << 22) + 7, 65, "bf16")):
+        l = torch.empty((N, A), dtype=TYPES[dtype], device="cuda").normal_()
+        ids = torch.randint(0, A, (N,), device="cuda", dtype=torch.int32)
+        f = dict(device="cuda")
+
+        def call(l, ids):
+            n = len(ids)
+            o = [torch.zeros(n, **f), torch.zeros(n, **f), torch.zeros((n, 2), **f),
+                 torch.zeros((n, 2), **f), torch.zeros((n, 2), dtype=torch.int32, **f)]
+            av.av_log_probs(l, ids, *o)
+            o.append(torch.zeros_like(l))
+            av.av_log_probs_backward(l, ids, o[2], o[1], o[0], o[0], o[5])
+            if A <= 256:
+                o.append(torch.zeros(n, dtype=torch.uint8, **f))
+                av.av_draw_actions(l, torch.sigmoid(o[0]), o[6])
+            return o
+        whole, tail = call(l, ids), call(l[-600:], ids[-600:])
+        # (another number of rows may take other kernels for long rows: sums in another order)
+        exact = A <= 2048
+        for a, b in zip(whole, tail):
+            a = a[-600:]
+            assert torch.equal(a, b) if exact else torch.allclose(a.float(), b.float(), atol=1e-4)
+        del whole, tail, l
+
+
 def test_more_alternatives_than_choices():
     logits, _ = some(4, 3, "f32")
     compare(logits, np.zeros(4, np.int64), "f32", top=5)

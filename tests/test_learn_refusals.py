@@ -25,7 +25,7 @@ def scan_config(**kw):
     return ctypes.byref(c)
 
 
-BAD_SCANS = [dict(steps=-1), dict(steps=1 << 31), dict(rows=-1), dict(width=0),
+BAD_SCANS = [dict(steps=-1), dict(steps=(1 << 30) + 1), dict(rows=1 << 14, width=(1 << 14) + 1), dict(rows=-1), dict(width=0),
              dict(rows=1 << 16, width=1 << 15), dict(rows=1 << 40, width=1 << 40), dict(dtype=3),
              dict(dtype=-1), dict(form=2), dict(reverse=2), dict(gate_per_value=-1),
              dict(x_step=1 << 60), dict(x_row=-8), dict(gate_step=-16)]
