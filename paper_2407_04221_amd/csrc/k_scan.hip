@@ -551,8 +551,9 @@ hipError_t pick(const ScanArgs &a, const ScanPlan &plan, bool gated, bool col, b
 template <typename T>
 hipError_t run(const ScanArgs &a, const ScanPlan &plan, bool gated, bool col, bool back,
                hipStream_t s) {
-    const hipError_t e = plan.vec > 1 ? pick<T, kWide<T>>(a, plan, gated, col, back, s)
-                                      : pick<T, 1>(a, plan, gated, col, back, s);
+    const hipError_t e = plan.vec == 1   ? pick<T, 1>(a, plan, gated, col, back, s)
+                         : plan.vec == 2 ? pick<T, 2>(a, plan, gated, col, back, s)
+                                         : pick<T, kWide<T>>(a, plan, gated, col, back, s);
     if (e != hipSuccess || !back || !col || !a.dgate) return e;
     // the workgroups' sums of a gate per value: [chunks * B][D] rows, first in runs, then all
     const int64_t m = int64_t(plan.chunks) * (a.N / a.D);
@@ -599,6 +600,11 @@ ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int wide, bool far, bool col
     if (T >= 8 && !far) {
         // words where they fill the device, or where chunks of time will have to anyway
         if (N / wide < int64_t(64) * kFill && N >= int64_t(64) * kFill / 2) plan.vec = 1;
+        if (plan.vec == 4 && N < int64_t(64) * kFill / 2) {
+            // of few groups a half empty one counts: smaller words where they waste less
+            const auto places = [&](int64_t V) { return (N / V + 63) / 64 * 64 * V; };
+            if (places(2) * 10 < places(4) * 9) plan.vec = 2;
+        }
         const int64_t K = steps_of(plan.vec), groups = scan_groups(N, plan.vec);
         const bool cut = groups < kFill / 2 && T > 3 * 8 * K;
         plan.waves = int(std::min<int64_t>(cut || groups > kFill / 2 ? 8 : waves_of(plan.vec),
