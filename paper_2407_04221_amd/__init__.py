@@ -458,18 +458,19 @@ def _types():
     return _known
 
 
-def _check_tensor(t, name, dtype, shape, device):
+def _refuse(t, name, dtype, shape, device):
     if not isinstance(t, _known[3]):
         raise TypeError(f"{name} must be a device tensor")
-    if t.dtype is not dtype or t.shape != shape or t.device != device:
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got "
-                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                     f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _operand(t, name, dtype, shape, device):
     """The address of a device tensor of this type, shape and device whose last dimension is
     contiguous, and its strides."""
-    _check_tensor(t, name, dtype, shape, device)
+    if not isinstance(t, _known[3]) or t.dtype is not dtype or t.shape != shape or \
+            t.device != device:
+        _refuse(t, name, dtype, shape, device)
     strides = t.stride()
     if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
@@ -480,7 +481,9 @@ def _packed(t, name, dtype, shape, device):
     """The address of a contiguous device tensor of this type, shape and device, or None."""
     if t is None:
         return None
-    _check_tensor(t, name, dtype, shape, device)
+    if not isinstance(t, _known[3]) or t.dtype is not dtype or t.shape != shape or \
+            t.device != device:
+        _refuse(t, name, dtype, shape, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
@@ -515,15 +518,19 @@ def _scan_common(x, gate, cut, form):
     shape, device, dtype = x.shape, x.device, x.dtype
     if shape[1] == 0 or shape[2] == 0:
         raise ValueError(f"an empty recurrence: x has shape {tuple(shape)}")
-    px, sx = _operand(x, "x", dtype, shape, device)
+    sx = x.stride()
+    if sx[2] != 1 and shape[2] > 1:
+        raise ValueError("the last dimension of x must be contiguous")
     per_value = gate.dim() == 1
     pg, sg = _operand(gate, "gate", dtype, shape[2:] if per_value else shape, device)
     pc, sc = None, (0, 0)
     if cut is not None:
-        _check_tensor(cut, "cut", torch.uint8, shape[:2], device)
+        if not isinstance(cut, tensor) or cut.dtype is not torch.uint8 or \
+                cut.shape != shape[:2] or cut.device != device:
+            _refuse(cut, "cut", torch.uint8, shape[:2], device)
         pc, sc = cut.data_ptr(), cut.stride()
-    return (floats[dtype], SCAN_FORMS[form] if isinstance(form, str) else int(form), px, sx, pg,
-            (0, 0) if per_value else sg, int(per_value), pc, sc)
+    return (floats[dtype], SCAN_FORMS[form] if isinstance(form, str) else int(form), x.data_ptr(),
+            sx, pg, (0, 0) if per_value else sg, 1 if per_value else 0, pc, sc)
 
 
 def av_scan_workspace(steps, rows, width, gate_per_value=False, backward=False, dtype=AV_F32) -> int:
