@@ -304,7 +304,11 @@ hipError_t launch_group_step(const StepArgs &a, hipStream_t s);
 // first.  first / final: the state (or its gradient) before the first processed step and after
 // the last one.
 struct ScanArgs {
-    int64_t T, N, D, chunk;           // steps, columns B x D, width, steps per chunk
+    int64_t T, N, D, chunk;           // steps, columns, columns of a row, steps per chunk
+    int64_t width;                    // values that have a gate each (a gate per value)
+    int64_t lanes, places;            // lanes of a row, and of all rows (the launcher's)
+    int runs;                         // runs of rows in the first sum of a gate per value
+    bool each;                        // cut has a flag for every column and not for every row
     const void *x, *gate, *y, *dy;
     const uint8_t *cut;
     const float *first, *h0;          // h0: the state itself, which the gradient of a gate needs
@@ -316,13 +320,16 @@ struct ScanArgs {
         dgate_step, dgate_row, cut_step, cut_row;
 };
 struct ScanPlan {
-    int vec, waves, chunks, runs;     // columns a lane; waves a workgroup (0: a lane takes its
-                                      // columns through all steps); chunks of time; runs of rows
-                                      // in the first sum of a gate per value
+    int vec, waves, chunks;           // columns a lane; waves a workgroup (0: a lane takes its
+                                      // columns through all steps); chunks of time
     int64_t chunk;                    // steps
-    size_t part_off, bytes;           // workspace: slots, then the sums
 };
-ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int wide, bool far, bool col, bool back);
+ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far);
+struct ScanSpace {
+    size_t part_off, bytes;           // the sums of a gate per value, and all of the workspace
+    int runs;
+};
+ScanSpace scan_space(const ScanPlan &plan, int64_t N, int64_t width, bool sums);
 hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool gated, bool col,
                        bool back, hipStream_t s);
 

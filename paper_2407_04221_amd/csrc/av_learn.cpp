@@ -100,11 +100,6 @@ bool reachable(int64_t step, int64_t n) {
     return step >= 0 && __int128(step) * n < (__int128(1) << 60);
 }
 
-// Whether groups of n neighbouring values are aligned words throughout.
-bool whole(const Place &a, size_t size, int n) {
-    return reinterpret_cast<uintptr_t>(a.p) % (n * size) == 0 && a.step % n == 0 && a.row % n == 0;
-}
-
 av_status check_workspace(const void *workspace, size_t bytes, size_t needed) {
     if (needed == 0) return AV_OK;
     if (!workspace || bytes < needed)
@@ -113,12 +108,15 @@ av_status check_workspace(const void *workspace, size_t bytes, size_t needed) {
     return AV_OK;
 }
 
+// The most that any layout of these sizes takes: rows apart, or as one, or far apart.
 size_t workspace_of(const av_scan_config &c, bool back) {
+    const int64_t N = c.rows * c.width;
+    const bool sums = back && c.gate_per_value;
     size_t most = 0;
-    for (int wide : {1, int(8 / size_of(c.dtype))})
-        if (c.width % wide == 0)
-            most = std::max(most, scan_plan(c.steps, c.rows, c.width, wide, false,
-                                            c.gate_per_value != 0, back).bytes);
+    for (const ScanPlan &plan : {scan_plan(c.steps, c.rows, c.width, c.dtype, false),
+                                 scan_plan(c.steps, 1, N, c.dtype, false),
+                                 scan_plan(c.steps, c.rows, c.width, c.dtype, true)})
+        most = std::max(most, scan_space(plan, N, c.width, sums).bytes);
     return most;
 }
 
@@ -136,9 +134,9 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     Place py = place(y, c.y_step, c.y_row), pdy = place(dy, c.dy_step, c.dy_row);
     Place po = back ? place(out, c.dx_step, c.dx_row) : place(out, c.y_step, c.y_row);
     Place pdg = place(dgate, c.dgate_step, c.dgate_row);
-    const Place everything[] = {px, pg, py, pdy, po, pdg, place(cut, c.cut_step, c.cut_row)};
-    for (const Place &a : everything)
-        if (a.p && (!reachable(a.step, c.steps) || !reachable(a.row, c.rows)))
+    Place pc = place(cut, c.cut_step, c.cut_row);
+    for (const Place *a : {&px, &pg, &py, &pdy, &po, &pdg, &pc})
+        if (a->p && (!reachable(a->step, c.steps) || !reachable(a->row, c.rows)))
             return bad("a stride is out of range");
     if (!spread(po.step, po.row, c)) return bad("strides of %s overlap its elements", back ? "dx" : "y");
     if (back && dgate && !col && !spread(pdg.step, pdg.row, c))
@@ -152,23 +150,23 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     for (const float *p : floats)
         if (reinterpret_cast<uintptr_t>(p) % 4) return bad("a state is not aligned to its type");
 
-    int wide = int(8 / size);
-    bool words = c.width % wide == 0 && whole(po, size, wide);
-    if (reads_x) words = words && whole(px, size, wide);
-    if (col) words = words && reinterpret_cast<uintptr_t>(gate) % 8 == 0;
-    else words = words && whole(pg, size, wide);
-    if (back) words = words && whole(py, size, wide) && whole(pdy, size, wide);
-    if (back && dgate && !col) words = words && whole(pdg, size, wide);
-    for (const float *p : floats) words = words && reinterpret_cast<uintptr_t>(p) % 16 == 0;
-    if (!words) wide = 1;
+    // rows that lie one behind the other are one long row, if no flags tell them apart or each
+    // value has its own
+    const bool each = cut && c.width == 1 && c.rows > 1 && c.cut_row == 1;
+    bool merge = c.rows > 1 && (!cut || each);
+    for (const Place *a : {&px, &pg, &py, &pdy, &po, &pdg})
+        if (a->p && !(col && (a == &pg || a == &pdg))) merge = merge && a->row == c.width;
+    const int64_t rows = merge ? 1 : c.rows, width = merge ? c.rows * c.width : c.width;
+    if (merge)
+        for (Place *a : {&px, &pg, &py, &pdy, &po, &pdg}) a->row = 0;
 
-    // a wave reaches the rows of its columns by 32-bit distances
-    const int64_t span = std::min(c.rows, 64 * wide / c.width + 2);
+    // a wave reaches the rows of its columns by 32-bit distances (64 lanes of up to 4 columns)
+    const int64_t span = std::min(rows, 4 * 64 / width + 2);
     bool far = false;
-    for (const Place &a : everything)
-        if (a.p) far = far || span * a.row + c.width >= (int64_t(1) << 32) / int64_t(size);
-
-    ScanPlan plan = scan_plan(c.steps, c.rows, c.width, wide, far, col, back);
+    for (const Place *a : {&px, &pg, &py, &pdy, &po, &pdg, &pc})
+        if (a->p) far = far || span * a->row + width >= (int64_t(1) << 32) / int64_t(size);
+    const ScanPlan plan = scan_plan(c.steps, rows, width, c.dtype, far);
+    const ScanSpace space = scan_space(plan, c.rows * c.width, c.width, back && col);
     if (some) {
         if (av_status st = check_workspace(workspace, workspace_bytes, workspace_of(c, back)))
             return st;
@@ -185,7 +183,8 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
         return q;
     };
     ScanArgs a{};
-    a.T = c.steps; a.N = c.rows * c.width; a.D = c.width; a.chunk = plan.chunk;
+    a.T = c.steps; a.N = rows * width; a.D = width; a.width = c.width; a.chunk = plan.chunk;
+    a.each = merge && each; a.runs = space.runs;
     a.x = turn(px.p, px.step, size); a.x_step = px.step; a.x_row = px.row;
     a.gate = col ? gate : turn(pg.p, pg.step, size);
     a.gate_step = pg.step; a.gate_row = pg.row;
@@ -194,13 +193,12 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     a.out = turn(po.p, po.step, size); a.out_step = po.step; a.out_row = po.row;
     a.dgate = col ? dgate : turn(pdg.p, pdg.step, size);
     a.dgate_step = pdg.step; a.dgate_row = pdg.row;
-    Place pc = place(cut, c.cut_step, c.cut_row);
     a.cut = reinterpret_cast<const uint8_t *>(turn(pc.p, pc.step, 1));
     a.cut_step = pc.step; a.cut_row = pc.row;
     a.first = first; a.h0 = h0; a.final = final;
     a.slots = some && plan.chunks > 1 ? workspace : nullptr;
     a.part = back && col && dgate && some
-                 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.part_off)
+                 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + space.part_off)
                  : nullptr;
     OnDevice on(c.device);
     if (on.error() != hipSuccess) return launched("hipSetDevice", on.error());

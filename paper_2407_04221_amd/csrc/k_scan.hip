@@ -48,35 +48,65 @@ __device__ inline float follow(float2 span, float s) {
     return span.x != span.x ? span.y : fmaf(span.x, s, span.y);
 }
 
-// V states of neighbouring columns, moved as words of up to 16 bytes.
-template <int V> struct alignas(V >= 4 ? 16 : 4) States { float v[V]; };
+// V neighbouring elements.  Global memory takes an access of up to 16 bytes at any address, so one
+// of V elements needs no more alignment than its element's.
+template <typename T, int V> struct Word { T v[V]; };
+typedef uint64_t Any2 __attribute__((ext_vector_type(2)));
+template <int kBytes> struct Bits;
+template <> struct Bits<1> { typedef uint8_t type; };
+template <> struct Bits<2> { typedef uint16_t type __attribute__((aligned(1))); };
+template <> struct Bits<4> { typedef uint32_t type __attribute__((aligned(1))); };
+template <> struct Bits<8> { typedef uint64_t type __attribute__((aligned(1))); };
+template <> struct Bits<16> { typedef Any2 type __attribute__((aligned(1))); };
 
-template <int V> __device__ inline States<V> states_at(const float *p, int64_t n) {
-    States<V> s;
-    if (p) {
-        s = *reinterpret_cast<const States<V> *>(p + n);
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) s.v[v] = 0.0f;
-    }
-    return s;
+template <typename E> __device__ inline E load_any(const void *p) {
+    const typename Bits<sizeof(E)>::type u =
+        *static_cast<const typename Bits<sizeof(E)>::type *>(p);
+    E e;
+    __builtin_memcpy(&e, &u, sizeof e);
+    return e;
 }
 
-// A lane's place: its first column n = b D + d, and whether it has one (a lane past the end
-// repeats the last columns and stores nothing).
+// A lane's place: V columns of row b from value d on, n = b D + d counted over all rows.  A row takes
+// lanes of V columns each; its last lane's start where V are left, so that `skip` of them are
+// the lane before's too: it works on them but stores nothing of them.  A lane past the end repeats
+// the last one's place and stores nothing.
 struct Column {
-    int n;
+    int n, skip;
     bool live;
     uint32_t b, d;
+    bool odd;                         // some lane of the wave skips columns
 };
 
 template <int V> __device__ inline Column column_of(const ScanArgs &p, int64_t place) {
     Column c;
-    c.live = place * V < p.N;
-    c.n = int(c.live ? place * V : p.N - V);
-    c.b = uint32_t(c.n) / uint32_t(p.D);
-    c.d = uint32_t(c.n) - c.b * uint32_t(p.D);
+    const uint32_t lanes = uint32_t(p.lanes);                 // of a row
+    c.live = place < p.places;
+    const uint32_t at = uint32_t(c.live ? place : p.places - 1);
+    c.b = at / lanes;
+    const uint32_t from = (at - c.b * lanes) * V;
+    c.d = min(from, uint32_t(p.D) - V);
+    c.skip = int(from - c.d);
+    c.n = int(c.b * uint32_t(p.D) + c.d);
+    c.odd = V > 1 && __ballot(c.skip != 0) != 0;
     return c;
+}
+
+// V states of neighbouring columns.
+template <int V> __device__ inline Word<float, V> states_at(const float *p, const Column &c) {
+    Word<float, V> s{};
+    if (p) s = load_any<Word<float, V>>(p + c.n);
+    return s;
+}
+template <int V, typename T> __device__ inline void put_states(T *p, const Column &c,
+                                                               const T (&v)[V]) {
+    if (!c.odd || c.skip == 0) {
+        __builtin_memcpy(p + c.n, v, sizeof v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= c.skip) p[c.n + i] = v[i];
+    }
 }
 
 // The workgroup's group of columns.  Workgroups are dealt to the 8 XCDs in turn; here each XCD takes
@@ -87,11 +117,6 @@ __device__ inline int64_t group_of_columns() {
     const uint32_t eighth = gridDim.x / 8, x = blockIdx.x;
     return gridDim.x % 8 ? x : x % 8 * eighth + x / 8;
 }
-
-template <int kBytes> struct Bits;
-template <> struct Bits<2> { typedef uint16_t type; };
-template <> struct Bits<4> { typedef uint32_t type; };
-template <> struct Bits<8> { typedef uint64_t type; };
 
 // A tensor as one workgroup sees it: a base and a step stride in bytes that are the same for the
 // whole wave, and the lane's own distance, which the host has made sure fits 32 bits; an access
@@ -110,40 +135,56 @@ struct Lanes {
         const char *p;
         int64_t step;
         uint32_t off;
-        template <typename E> __device__ E get() const { return *reinterpret_cast<const E *>(p + off); }
+        template <typename E> __device__ E get() const { return load_any<E>(p + off); }
         // Written past the caches: outputs are not read again by the kernel, and the inputs that
-        // other workgroups still want stay.
-        template <typename E> __device__ void put(const E &e) const {
-            typedef typename Bits<sizeof(E)>::type U;
-            U u;
-            __builtin_memcpy(&u, &e, sizeof u);
-            __builtin_nontemporal_store(u, reinterpret_cast<U *>(const_cast<char *>(p) + off));
+        // other workgroups still want stay (65536 x 2 x 320 in f16 both ways: 188 us, without 202).
+        // c.odd is the same for the wave, so that most waves never look at their lanes' skip.
+        template <typename T, int V> __device__ void put(const Word<T, V> &e, const Column &c) const {
+            typedef typename Bits<sizeof(T) * V>::type U;
+            char *to = const_cast<char *>(p) + off;
+            if (!c.odd || c.skip == 0) {
+                U u;
+                __builtin_memcpy(&u, &e, sizeof u);
+                __builtin_nontemporal_store(u, reinterpret_cast<U *>(to));
+            } else {
+                typedef typename Bits<sizeof(T)>::type One;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    One one;
+                    __builtin_memcpy(&one, &e.v[v], sizeof one);
+                    if (v >= c.skip)
+                        __builtin_nontemporal_store(one, reinterpret_cast<One *>(to) + v);
+                }
+            }
         }
         __device__ void next() { p += step; }
     };
     __device__ Cursor at(int q) const { return Cursor{base + q * step, step, off}; }
 };
 
-// K consecutive steps of V columns as they come from memory.
-template <typename T, int V, int K, bool kX, bool kGate, bool kBack> struct Raw {
-    Vec<T, V> e[K], g[kGate ? K : 1], x[kX ? K : 1], before[kBack ? K : 1];
-    uint8_t cut[K];
+// K consecutive steps of V columns as they come from memory; kEach: with V flags, one for
+// each column.
+template <typename T, int V, int K, bool kX, bool kGate, bool kBack, bool kEach> struct Raw {
+    Word<T, V> e[K], g[kGate ? K : 1], x[kX ? K : 1], before[kBack ? K : 1];
+    Word<uint8_t, kEach ? V : 1> cut[K];
 };
 
 // The same in 32 bits: a step takes the state s to a s + b (to b where it is cut), with
 // b = x or (1 - a) x, or, in the gradient, c to a (c + e) (to 0), e the gradient of the output.
-template <int V, int K, bool kRest> struct Work {
+template <int V, int K, bool kRest, bool kEach> struct Work {
     float a[K][V], b[K][V], rest[kRest ? K : 1][V];
-    uint8_t cut[K];
+    Word<uint8_t, kEach ? V : 1> flags[K];
+    __device__ bool cut(int k, int v) const { return flags[k].v[kEach ? v : 0] != 0; }
 };
 
 // One direction's view of the tensors.  kBack: e is dy, `before` the state before the step, and x is
 // read only where gated; else e is x.
-template <typename T, int V, int K, bool kGated, bool kCol, bool kBack> struct Reader {
+template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEach> struct Reader {
     static constexpr bool kX = kBack && kGated, kRest = kBack && kGated;
-    using In = Raw<T, V, K, kX, !kCol, kBack>;
-    using Out = Work<V, K, kRest>;
-    using Values = Vec<T, V>;
+    using In = Raw<T, V, K, kX, !kCol, kBack, kEach>;
+    using Out = Work<V, K, kRest, kEach>;
+    using Values = Word<T, V>;
+    using Flags = Word<uint8_t, kEach ? V : 1>;
     Lanes x, g, e, y, cut;
     int steps;
     bool cuts;
@@ -153,13 +194,13 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack> struct R
         : x(p.x, p.x_step, p.x_row, sizeof(T), b0, c), g(p.gate, p.gate_step, p.gate_row, sizeof(T), b0, c, !kCol),
           e(kBack ? p.dy : p.x, kBack ? p.dy_step : p.x_step, kBack ? p.dy_row : p.x_row, sizeof(T), b0, c),
           y(p.y, p.y_step, p.y_row, sizeof(T), b0, c),
-          cut(p.cut, p.cut_step, p.cut_row, 1, b0, Column{c.n, c.live, c.b, 0}), steps(int(p.T)),
+          cut(p.cut, p.cut_step, p.cut_row, 1, b0, Column{c.n, 0, c.live, c.b, p.each ? c.d : 0, false}), steps(int(p.T)),
           cuts(p.cut != nullptr) {
         if (kCol) {
-            const Values v = g.at(0).template get<Values>();
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                ca[i] = to_f32(v.v[i]);
+                const uint32_t d = uint32_t(c.n + i) % uint32_t(p.width);
+                ca[i] = to_f32(static_cast<const T *>(p.gate)[d]);
                 cr[i] = 1.0f;
                 if (kGated) gate_pair(ca[i], ca[i], cr[i]);
             }
@@ -189,12 +230,12 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack> struct R
         if (cuts) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                r.cut[k] = pc.template get<uint8_t>();
+                r.cut[k] = pc.template get<Flags>();
                 if (whole || q + k + 1 < end) pc.next();
             }
         } else {
 #pragma unroll
-            for (int k = 0; k < K; ++k) r.cut[k] = 0;
+            for (int k = 0; k < K; ++k) r.cut[k] = Flags{};
         }
     }
 
@@ -202,7 +243,7 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack> struct R
     __device__ void unpack(const In &r, int n, Out &o) const {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            o.cut[k] = r.cut[k];
+            o.flags[k] = r.cut[k];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float a = ca[v], rest = cr[v];
@@ -221,7 +262,7 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack> struct R
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 if (k < n) continue;
-                o.cut[k] = 0;
+                o.flags[k] = Flags{};
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     o.a[k][v] = 1.0f;
@@ -238,37 +279,37 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack> struct R
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (kBack) s[v].y = o.cut[k] ? 0.0f : o.a[k][v] * (s[v].y + o.b[k][v]);
-                else s[v].y = o.cut[k] ? o.b[k][v] : fmaf(o.a[k][v], s[v].y, o.b[k][v]);
-                s[v].x = o.cut[k] ? __builtin_nanf("") : s[v].x * o.a[k][v];
+                if (kBack) s[v].y = o.cut(k, v) ? 0.0f : o.a[k][v] * (s[v].y + o.b[k][v]);
+                else s[v].y = o.cut(k, v) ? o.b[k][v] : fmaf(o.a[k][v], s[v].y, o.b[k][v]);
+                s[v].x = o.cut(k, v) ? __builtin_nanf("") : s[v].x * o.a[k][v];
             }
     }
 
     // Takes V states through step k: the output, and the gradient of the gate.  first: this is the
     // recurrence's first step (the gradient's last), whose state before is h.
-    static __device__ void step(const In &r, const Out &o, int k, bool first, const States<V> &h,
+    static __device__ void step(const In &r, const Out &o, int k, bool first, const Word<float, V> &h,
                                 float (&state)[V], float (&out)[V], float (&dgate)[V]) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float a = o.a[k][v];
             if (kBack) {
                 const float lam = o.b[k][v] + state[v];
-                state[v] = o.cut[k] ? 0.0f : a * lam;
+                state[v] = o.cut(k, v) ? 0.0f : a * lam;
                 float s = first ? h.v[v] : to_f32(r.before[k].v[v]);
-                s = o.cut[k] ? 0.0f : s;
+                s = o.cut(k, v) ? 0.0f : s;
                 out[v] = kGated ? lam * o.rest[k][v] : lam;
                 // lam (s - x) a (1 - a), or lam s
                 dgate[v] = kGated ? out[v] * a * (s - to_f32(r.x[k].v[v])) : lam * s;
             } else {
-                state[v] = o.cut[k] ? o.b[k][v] : fmaf(a, state[v], o.b[k][v]);
+                state[v] = o.cut(k, v) ? o.b[k][v] : fmaf(a, state[v], o.b[k][v]);
                 out[v] = state[v];
             }
         }
     }
 };
 
-template <typename T, int V> __device__ inline Vec<T, V> rounded(const float (&f)[V]) {
-    Vec<T, V> o;
+template <typename T, int V> __device__ inline Word<T, V> rounded(const float (&f)[V]) {
+    Word<T, V> o;
 #pragma unroll
     for (int v = 0; v < V; ++v) o.v[v] = from_f32<T>(f[v]);
     return o;
@@ -276,14 +317,14 @@ template <typename T, int V> __device__ inline Vec<T, V> rounded(const float (&f
 
 // First kernel of a recurrence cut into chunks: slot 0 of the workspace takes the state coming in
 // (as a span that gives it), slot s + 1 the span of chunk s.
-template <typename T, int V, bool kGated, bool kCol, bool kBack>
+template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
 __global__ void __launch_bounds__(64 * waves_of(V)) scan_chunks_kernel(ScanArgs p) {
     constexpr int K = steps_of(V);
     __shared__ float2 spans[waves_of(V) * 64 * V];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int W = blockDim.x >> 6;
     const Column c = column_of<V>(p, group_of_columns() * 64 + lane);
-    using R = Reader<T, V, K, kGated, kCol, kBack>;
+    using R = Reader<T, V, K, kGated, kCol, kBack, kEach>;
     const R in(p, c, __builtin_amdgcn_readfirstlane(c.b));
     const int begin = int(blockIdx.y) * int(p.chunk), part = int(p.chunk) / W;
     float2 total[V];
@@ -308,20 +349,22 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_chunks_kernel(ScanArgs 
     __syncthreads();
     if (w != 0 || !c.live) return;
     float2 *slots = static_cast<float2 *>(p.slots);
+    const Word<float, V> first = states_at<V>(p.first, c);
+    float2 mine[V], start[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        float2 s = spans[lane * V + v];
+        mine[v] = spans[lane * V + v];
         for (int j = 1; j < W; ++j) {
             const float2 next = spans[(j * 64 + lane) * V + v];
-            s = make_float2(next.x * s.x, follow(next, s.y));
+            mine[v] = make_float2(next.x * mine[v].x, follow(next, mine[v].y));
         }
-        slots[int64_t(blockIdx.y + 1) * p.N + c.n + v] = s;
-        if (blockIdx.y == 0)
-            slots[c.n + v] = make_float2(__builtin_nanf(""), p.first ? p.first[c.n + v] : 0.0f);
+        start[v] = make_float2(__builtin_nanf(""), first.v[v]);
     }
+    put_states(slots + int64_t(blockIdx.y + 1) * p.N, c, mine);
+    if (blockIdx.y == 0) put_states(slots, c, start);
 }
 
-template <typename T, int V, bool kGated, bool kCol, bool kBack>
+template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
 __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     constexpr int K = steps_of(V), kMost = waves_of(V);
     // Loading a tile ahead pays where few workgroups share a compute unit; with many it only
@@ -332,7 +375,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int W = blockDim.x >> 6;
     const Column c = column_of<V>(p, group_of_columns() * 64 + lane);
-    using R = Reader<T, V, K, kGated, kCol, kBack>;
+    using R = Reader<T, V, K, kGated, kCol, kBack, kEach>;
     const uint32_t b0 = __builtin_amdgcn_readfirstlane(c.b);
     const R in(p, c, b0);
     // fewer than 2^31 steps: kMost K more do not pass 32 bits unsigned
@@ -340,7 +383,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     const int end = int(min(p.T, begin + p.chunk)), tile = W * K;
     typename R::In next;
     if (kAhead) in.template load<false>(next, begin + w * K, end);
-    const States<V> h = states_at<V>(kBack ? p.h0 : nullptr, c.n);
+    const Word<float, V> h = states_at<V>(kBack ? p.h0 : nullptr, c);
     float state[V];
     int par = 0;
     if (p.slots) {
@@ -366,7 +409,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
 #pragma unroll
             for (int v = 0; v < V; ++v) state[v] = follow(spans[1][(j * 64 + lane) * V + v], state[v]);
     } else {
-        const States<V> first = states_at<V>(p.first, c.n);
+        const Word<float, V> first = states_at<V>(p.first, c);
 #pragma unroll
         for (int v = 0; v < V; ++v) state[v] = first.v[v];
     }
@@ -407,8 +450,8 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
             float o[V], dg[V];
             R::step(raw, work, k, q + k == in.steps - 1, h, state, o, dg);
             if (k < n) {                      // the others change nothing and are no one's output
-                if (c.live) po.put(rounded<T, V>(o));
-                if (with_gate && c.live) pg.put(rounded<T, V>(dg));
+                if (c.live) po.put(rounded<T, V>(o), c);
+                if (with_gate && c.live) pg.put(rounded<T, V>(dg), c);
                 if (kBack && kCol) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) sum[v] += dg[v];
@@ -423,10 +466,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
         }
     }
     // the last wave went through every step (those past the end change nothing)
-    if (p.final && w == W - 1 && c.live && end == in.steps) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) p.final[c.n + v] = state[v];
-    }
+    if (p.final && w == W - 1 && c.live && end == in.steps) put_states(p.final, c, state);
     if (kBack && kCol && p.part) {
         __syncthreads();
         float *red = reinterpret_cast<float *>(spans);
@@ -435,25 +475,23 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
         __syncthreads();
         if (w == 0 && c.live) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float s = sum[v];
-                for (int j = 1; j < W; ++j) s += red[(j * 64 + lane) * V + v];
-                p.part[int64_t(blockIdx.y) * p.N + c.n + v] = s;
-            }
+            for (int v = 0; v < V; ++v)
+                for (int j = 1; j < W; ++j) sum[v] += red[(j * 64 + lane) * V + v];
+            put_states(p.part + int64_t(blockIdx.y) * p.N, c, sum);
         }
     }
 }
 
 // A few steps (an agent's acting step is one): a lane takes its columns through all of them.  Its
 // addresses are 64 bits a lane, so any distance between rows will do.
-template <typename T, int V, bool kGated, bool kCol, bool kBack>
+template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
 __global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs p) {
     const Column c = column_of<V>(p, int64_t(blockIdx.x) * 256 + threadIdx.x);
     if (!c.live) return;
-    using R = Reader<T, V, 1, kGated, kCol, kBack>;
+    using R = Reader<T, V, 1, kGated, kCol, kBack, kEach>;
     const R in(p, c, c.b);
-    const States<V> h = states_at<V>(kBack ? p.h0 : nullptr, c.n);
-    States<V> state = states_at<V>(p.first, c.n);
+    const Word<float, V> h = states_at<V>(kBack ? p.h0 : nullptr, c);
+    Word<float, V> state = states_at<V>(p.first, c);
     const Lanes out(p.out, p.out_step, p.out_row, sizeof(T), c.b, c);
     const Lanes dgate(p.dgate, p.dgate_step, p.dgate_row, sizeof(T), c.b, c);
     float sum[V] = {};
@@ -464,16 +502,13 @@ __global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs p) {
         in.unpack(raw, 1, work);
         float o[V], dg[V];
         R::step(raw, work, 0, q == in.steps - 1, h, state.v, o, dg);
-        out.at(q).put(rounded<T, V>(o));
-        if (kBack && !kCol && p.dgate) dgate.at(q).put(rounded<T, V>(dg));
+        out.at(q).put(rounded<T, V>(o), c);
+        if (kBack && !kCol && p.dgate) dgate.at(q).put(rounded<T, V>(dg), c);
 #pragma unroll
         for (int v = 0; v < V; ++v) sum[v] += kBack && kCol ? dg[v] : 0.0f;
     }
-    if (p.final) *reinterpret_cast<States<V> *>(p.final + c.n) = state;
-    if (kBack && kCol && p.part) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) p.part[c.n + v] = sum[v];
-    }
+    if (p.final) put_states(p.final, c, state.v);
+    if (kBack && kCol && p.part) put_states(p.part, c, sum);
 }
 
 // Sums m rows of `width` floats into one row (to type T): a workgroup takes `lanes` values, its
@@ -510,42 +545,54 @@ __global__ void __launch_bounds__(256) zero_kernel(T *dst, int n) {
     if (i < n) dst[i] = from_f32<T>(0.0f);
 }
 
+// Lanes that B rows of D values take, V columns each.
+int64_t scan_places(int64_t B, int64_t D, int V) { return B * ((D + V - 1) / V); }
+
 // Workgroups over the columns; from 64 on a multiple of 8 (group_of_columns), the last ones empty.
-unsigned scan_groups(int64_t N, int V) {
-    const int64_t n = (N / V + 63) / 64;
+unsigned scan_groups(int64_t places) {
+    const int64_t n = (places + 63) / 64;
     return unsigned(n < 64 ? n : (n + 7) / 8 * 8);
 }
 
-template <typename T, int V, bool kGated, bool kCol, bool kBack>
-hipError_t launch(const ScanArgs &a, const ScanPlan &plan, hipStream_t s) {
+template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
+hipError_t launch(const ScanArgs &all, const ScanPlan &plan, hipStream_t s) {
+    ScanArgs a = all;
+    a.lanes = scan_places(1, a.D, V);
+    a.places = a.N / a.D * a.lanes;
     if (plan.waves == 0) {
-        const unsigned blocks = unsigned((a.N / V + 255) / 256);
-        hipLaunchKernelGGL((scan_short_kernel<T, V, kGated, kCol, kBack>), dim3(blocks), dim3(256),
+        const unsigned blocks = unsigned((a.places + 255) / 256);
+        hipLaunchKernelGGL((scan_short_kernel<T, V, kGated, kCol, kBack, kEach>), dim3(blocks), dim3(256),
                            0, s, a);
         return hipGetLastError();
     }
-    const unsigned groups = scan_groups(a.N, V);
+    const unsigned groups = scan_groups(a.places);
     if (plan.chunks > 1)
-        hipLaunchKernelGGL((scan_chunks_kernel<T, V, kGated, kCol, kBack>),
+        hipLaunchKernelGGL((scan_chunks_kernel<T, V, kGated, kCol, kBack, kEach>),
                            dim3(groups, plan.chunks - 1), dim3(64 * plan.waves), 0, s, a);
-    hipLaunchKernelGGL((scan_kernel<T, V, kGated, kCol, kBack>), dim3(groups, plan.chunks),
+    hipLaunchKernelGGL((scan_kernel<T, V, kGated, kCol, kBack, kEach>), dim3(groups, plan.chunks),
                        dim3(64 * plan.waves), 0, s, a);
     return hipGetLastError();
 }
 
-template <typename T, int V, bool kGated>
+template <typename T, int V, bool kGated, bool kEach>
 hipError_t pick(const ScanArgs &a, const ScanPlan &plan, bool col, bool back, hipStream_t s) {
     if (back)
-        return col ? launch<T, V, kGated, true, true>(a, plan, s)
-                   : launch<T, V, kGated, false, true>(a, plan, s);
-    return col ? launch<T, V, kGated, true, false>(a, plan, s)
-               : launch<T, V, kGated, false, false>(a, plan, s);
+        return col ? launch<T, V, kGated, true, true, kEach>(a, plan, s)
+                   : launch<T, V, kGated, false, true, kEach>(a, plan, s);
+    return col ? launch<T, V, kGated, true, false, kEach>(a, plan, s)
+               : launch<T, V, kGated, false, false, kEach>(a, plan, s);
 }
 
 template <typename T, int V>
 hipError_t pick(const ScanArgs &a, const ScanPlan &plan, bool gated, bool col, bool back,
                 hipStream_t s) {
-    return gated ? pick<T, V, true>(a, plan, col, back, s) : pick<T, V, false>(a, plan, col, back, s);
+    if constexpr (V > 1) {
+        if (a.each)
+            return gated ? pick<T, V, true, true>(a, plan, col, back, s)
+                         : pick<T, V, false, true>(a, plan, col, back, s);
+    }
+    return gated ? pick<T, V, true, false>(a, plan, col, back, s)
+                 : pick<T, V, false, false>(a, plan, col, back, s);
 }
 
 template <typename T>
@@ -556,20 +603,20 @@ hipError_t run(const ScanArgs &a, const ScanPlan &plan, bool gated, bool col, bo
                                          : pick<T, kWide<T>>(a, plan, gated, col, back, s);
     if (e != hipSuccess || !back || !col || !a.dgate) return e;
     // the workgroups' sums of a gate per value: [chunks * B][D] rows, first in runs, then all
-    const int64_t m = int64_t(plan.chunks) * (a.N / a.D);
-    const int D = int(a.D);
+    const int64_t m = int64_t(plan.chunks) * (a.N / a.width);
+    const int D = int(a.width);
     int lanes = 1;
     while (lanes < 16 && lanes < D) lanes *= 2;
     const unsigned blocks = unsigned((D + lanes - 1) / lanes);
     const float *src = a.part;
     int64_t rows = m;
-    if (plan.runs > 1) {
-        const int64_t each = (m + plan.runs - 1) / plan.runs;
+    if (a.runs > 1) {
+        const int64_t each = (m + a.runs - 1) / a.runs;
         float *mid = a.part + m * D;
-        hipLaunchKernelGGL((sum_rows_kernel<float>), dim3(blocks, plan.runs), dim3(1024), 0, s, src,
+        hipLaunchKernelGGL((sum_rows_kernel<float>), dim3(blocks, a.runs), dim3(1024), 0, s, src,
                            m, each, D, lanes, mid);
         src = mid;
-        rows = plan.runs;
+        rows = a.runs;
     }
     hipLaunchKernelGGL((sum_rows_kernel<T>), dim3(blocks, 1), dim3(1024), 0, s, src, rows, rows, D,
                        lanes, static_cast<T *>(a.dgate));
@@ -580,54 +627,61 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 
 }  // namespace
 
-// How the sizes are shared out.  wide: columns of an 8-byte word, 1 where accesses of words would
-// not all be aligned; far: rows too far apart for a wave's addressing.
+// How the sizes are shared out.  B rows of D values, all rows as one where they lie one behind the
+// other; far: rows too far apart for a wave's addressing.
+//   A lane takes a word of columns of up to 8 bytes, as long as that leaves at most a fifth of
+//   the lanes' columns to no one.  Odd widths too in 16 bits (30230 x 325 in bf16 both ways: 94 us,
+//   with single columns 109), but not in 32 (777 x 33 x 129: 42 us, with single columns 39).
 //   A few steps, or far rows: a lane takes its columns through all of them.
-//   Else a lane takes a word of columns where that still fills the device, for its longer row
-//   segments (128 x 1024 x 256 in bf16: 42 us forward, with single columns 50), and one column
-//   where only that does (2048 x 64 x 256: 58 us, with words 151).  Where neither does, time is cut
-//   into chunks, if there are more than three tiles of eight waves (below that the second launch
-//   costs more than the idle units), and words are taken again.
+//   Else words where they still fill the device, for their longer row segments (128 x 1024 x 256 in
+//   bf16: 42 us forward, with single columns 50), and one column where only that does (2048 x 64 x
+//   256: 58 us, with words 151).  Where neither does, and there are more than three tiles of sixteen
+//   waves of single columns (at some 2 us a tile; below that a second launch costs more), time is
+//   cut into chunks, and words are taken again, smaller ones where they leave fewer lanes idle
+//   (65536 x 2 x 320 in f16: 188 us both ways, with the longest 219).
 //   Waves: eight, or sixteen where there is at most one uncut workgroup a compute unit, which has to
 //   hide its own latency (1000 x 16384 in f32: 26.3 us, with eight 27.7; but 300 x 500 x 33, some
 //   units with two workgroups: 22.1 with sixteen, 18.4 with eight).
-ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int wide, bool far, bool col, bool back) {
+ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far) {
     ScanPlan plan{};
-    const int64_t N = B * D;
     plan.chunks = 1;
     plan.chunk = std::max<int64_t>(1, T);
-    plan.vec = wide;
-    if (T >= 8 && !far) {
-        // words where they fill the device, or where chunks of time will have to anyway
-        if (N / wide < int64_t(64) * kFill && N >= int64_t(64) * kFill / 2) plan.vec = 1;
-        if (plan.vec == 4 && N < int64_t(64) * kFill / 2) {
-            // of few groups a half empty one counts: smaller words where they waste less
-            const auto places = [&](int64_t V) { return (N / V + 63) / 64 * 64 * V; };
-            if (places(2) * 10 < places(4) * 9) plan.vec = 2;
-        }
-        const int64_t K = steps_of(plan.vec), groups = scan_groups(N, plan.vec);
-        const bool cut = groups < kFill / 2 && T > 3 * 8 * K;
-        plan.waves = int(std::min<int64_t>(cut || groups > kFill / 2 ? 8 : waves_of(plan.vec),
-                                           (T + K - 1) / K));
-        if (cut) {
-            const int64_t tile = plan.waves * K, tiles = (T + tile - 1) / tile;
-            const int64_t want = std::min((kFill + groups - 1) / groups, tiles);
-            plan.chunk = (tiles + want - 1) / want * tile;
-            plan.chunks = int((T + plan.chunk - 1) / plan.chunk);
-        }
+    plan.vec = dtype == AV_F32 ? 2 : 4;
+    while (plan.vec > 1 && (plan.vec > D || scan_places(1, D, plan.vec) * plan.vec * 4 > D * 5 ||
+                            (dtype == AV_F32 && D % plan.vec)))
+        plan.vec /= 2;
+    if (B == 0 || T < 8 || far) return plan;
+    const int64_t fill = int64_t(64) * kFill, N = B * D;
+    const bool cut = N < fill / 2 && T > 3 * 16 * steps_of(1);
+    if (!cut && scan_places(B, D, plan.vec) < fill) plan.vec = 1;
+    // columns that whole workgroups have room for
+    const auto room = [&](int64_t V) { return (scan_places(B, D, V) + 63) / 64 * 64 * V; };
+    while (cut && plan.vec > 1 && room(plan.vec / 2) * 10 < room(plan.vec) * 9) plan.vec /= 2;
+    const int64_t K = steps_of(plan.vec), groups = scan_groups(scan_places(B, D, plan.vec));
+    plan.waves = int(std::min<int64_t>(cut || groups > kFill / 2 ? 8 : waves_of(plan.vec),
+                                       (T + K - 1) / K));
+    if (cut) {
+        const int64_t tile = plan.waves * K, tiles = (T + tile - 1) / tile;
+        const int64_t want = std::min((kFill + groups - 1) / groups, tiles);
+        plan.chunk = (tiles + want - 1) / want * tile;
+        plan.chunks = int((T + plan.chunk - 1) / plan.chunk);
     }
-    size_t bytes = 0;
-    if (plan.chunks > 1) bytes = round16(size_t(plan.chunks) * size_t(N) * sizeof(float2));
-    plan.part_off = bytes;
-    plan.runs = 1;
-    if (back && col) {
-        const int64_t m = int64_t(plan.chunks) * B;
-        if (m > 1024) plan.runs = int(std::min<int64_t>(64, m / 256));
-        bytes += size_t(m) * size_t(D) * sizeof(float);
-        if (plan.runs > 1) bytes += size_t(plan.runs) * size_t(D) * sizeof(float);
-    }
-    plan.bytes = bytes;
     return plan;
+}
+
+// The workspace of a plan: the chunks' spans, then, for a gradient of `width` gates, the sums of them
+// that the workgroups leave: one row of `width` for each chunk and row of the recurrence.
+ScanSpace scan_space(const ScanPlan &plan, int64_t N, int64_t width, bool sums) {
+    ScanSpace space{0, 0, 1};
+    if (plan.chunks > 1) space.bytes = round16(size_t(plan.chunks) * size_t(N) * sizeof(float2));
+    space.part_off = space.bytes;
+    if (sums) {
+        const int64_t m = plan.chunks * (N / width);
+        if (m > 1024) space.runs = int(std::min<int64_t>(64, m / 256));
+        space.bytes += size_t(m) * size_t(width) * sizeof(float);
+        if (space.runs > 1) space.bytes += size_t(space.runs) * size_t(width) * sizeof(float);
+    }
+    return space;
 }
 
 hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool gated, bool col,
@@ -638,7 +692,7 @@ hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool 
             hipLaunchKernelGGL(copy_state_kernel, dim3(blocks), dim3(256), 0, s, a.first, a.final,
                                int(a.N));
         if (back && col && a.dgate) {
-            const int D = int(a.D);
+            const int D = int(a.width);
             const dim3 g(unsigned((D + 255) / 256));
             if (dtype == AV_F32)
                 hipLaunchKernelGGL((zero_kernel<float>), g, dim3(256), 0, s,

@@ -114,6 +114,24 @@ def test_words_of_columns(dtype, form, columns):
         run(T, 50, 24, reverse=T == 3, **kw)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("columns", [False, True])
+def test_rows_one_behind_the_other(dtype, columns):
+    """Rows that make one long row, a word of columns of several rows a lane: with a flag for each
+    value, without flags, and odd counts that rule it out."""
+    kw = dict(dtype=dtype, columns=columns)
+    for B in (4, 6, 7, 128, 130):
+        run(900, B, 1, reverse=True, cut=0.02, **kw)
+        run(5, B, 1, form="gated", cut=0.3, **kw)
+    run(600, 20, 3, cut=None, **kw)
+    run(600, 20, 3, cut=0.02, **kw)
+    run(500, 4, 6, cut=None, form="gated", reverse=True, **kw)
+    run(500, 8, 1, cut=0.02, layout="batch", **kw)
+    run(500, 8, 1, cut=0.02, pad=1, **kw)
+    run(12, 140000, 1, cut=0.1, **kw)
+    run(9, 40000, 5, cut=None, form="gated", **kw)
+
+
 @pytest.mark.parametrize("columns", [False, True])
 def test_single_columns_that_fill_the_device(columns):
     """One uncut workgroup of sixteen waves a compute unit, several tiles; then more workgroups."""
