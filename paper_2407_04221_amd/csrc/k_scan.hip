@@ -48,25 +48,6 @@ __device__ inline float follow(float2 span, float s) {
     return span.x != span.x ? span.y : fmaf(span.x, s, span.y);
 }
 
-// V neighbouring elements.  Global memory takes an access of up to 16 bytes at any address, so one
-// of V elements needs no more alignment than its element's.
-template <typename T, int V> struct Word { T v[V]; };
-typedef uint64_t Any2 __attribute__((ext_vector_type(2)));
-template <int kBytes> struct Bits;
-template <> struct Bits<1> { typedef uint8_t type; };
-template <> struct Bits<2> { typedef uint16_t type __attribute__((aligned(1))); };
-template <> struct Bits<4> { typedef uint32_t type __attribute__((aligned(1))); };
-template <> struct Bits<8> { typedef uint64_t type __attribute__((aligned(1))); };
-template <> struct Bits<16> { typedef Any2 type __attribute__((aligned(1))); };
-
-template <typename E> __device__ inline E load_any(const void *p) {
-    const typename Bits<sizeof(E)>::type u =
-        *static_cast<const typename Bits<sizeof(E)>::type *>(p);
-    E e;
-    __builtin_memcpy(&e, &u, sizeof e);
-    return e;
-}
-
 // A lane's place: V columns of row b from value d on, n = b D + d counted over all rows.  A row takes
 // lanes of V columns each; its last lane's start where V are left, so that `skip` of them are
 // the lane before's too: it works on them but stores nothing of them.  A lane past the end repeats
@@ -140,21 +121,13 @@ struct Lanes {
         // other workgroups still want stay (65536 x 2 x 320 in f16 both ways: 188 us, without 202).
         // c.odd is the same for the wave, so that most waves never look at their lanes' skip.
         template <typename T, int V> __device__ void put(const Word<T, V> &e, const Column &c) const {
-            typedef typename Bits<sizeof(T) * V>::type U;
             char *to = const_cast<char *>(p) + off;
             if (!c.odd || c.skip == 0) {
-                U u;
-                __builtin_memcpy(&u, &e, sizeof u);
-                __builtin_nontemporal_store(u, reinterpret_cast<U *>(to));
+                store_past(to, e);
             } else {
-                typedef typename Bits<sizeof(T)>::type One;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    One one;
-                    __builtin_memcpy(&one, &e.v[v], sizeof one);
-                    if (v >= c.skip)
-                        __builtin_nontemporal_store(one, reinterpret_cast<One *>(to) + v);
-                }
+                for (int v = 0; v < V; ++v)
+                    if (v >= c.skip) store_past(to + v * sizeof(T), e.v[v]);
             }
         }
         __device__ void next() { p += step; }

@@ -10,8 +10,8 @@
 // t 2^t so that its 0 is not -inf x 0.  A NaN or +inf among the logits makes S a NaN.
 //
 // One pass over the logits: each thread keeps its own (m, S, w) and rescales S and w when its m
-// grows.  A thread takes a whole row of up to 16 choices, a wave of up to kWaveRow, else a
-// workgroup.  Rows are read as aligned 16-byte words, the row's two ends element by element.
+// grows.  A thread takes a whole row of up to 16 choices, 4 to 64 lanes one of up to kWaveRow, else
+// a workgroup, or several.  Longer rows are read as 16-byte words wherever they start.
 #include <algorithm>
 
 #include "av_internal.h"
@@ -278,33 +278,44 @@ __global__ void __launch_bounds__(256) small_back_kernel(TokenArgs a) {
     }
 }
 
-// ---- longer rows, as aligned words of kPer elements ----
+// ---- longer rows, as words of kPer elements (16 bytes, at any address) ----
 
+// A row's last word starts where kPer elements are left, so its first `skip` elements are the word
+// before's too: they count as masked and are not stored.  The row has at least kPer.
 template <typename T> struct Words {
     static constexpr int kPer = 16 / sizeof(T);
     const T *l;
-    int skip, A, count;         // elements of the first word before the row, and words of the row
+    int A, count;
 
     __device__ Words(const TokenArgs &a, int64_t row)
-        : l(static_cast<const T *>(a.logits) + row * a.stride), A(a.A) {
-        skip = int(reinterpret_cast<uintptr_t>(l) / sizeof(T) % kPer);
-        count = int((int64_t(skip) + A + kPer - 1) / kPer);
+        : l(static_cast<const T *>(a.logits) + row * a.stride), A(a.A),
+          count((a.A + kPer - 1) / kPer) {}
+    __device__ int first(int word) const { return min(word * kPer, A - kPer); }
+    __device__ int skip(int word) const { return word * kPer - first(word); }
+    __device__ Word<T, kPer> get(int word) const {
+        return load_any<Word<T, kPer>>(l + first(word));
     }
-    __device__ int first(int word) const { return word * kPer - skip; }
-    __device__ bool whole(int word) const {
-        return word < count && first(word) >= 0 && int64_t(first(word)) + kPer <= A;
-    }
-    // Elements first(word) .. + kPer - 1; -inf outside the row.
+    // Elements first(word) .. + kPer - 1; -inf where skipped, and all where there is no such word.
     __device__ void load(int word, float (&v)[kPer]) const {
-        const int at = first(word);
-        if (whole(word)) {
-            const Vec<T, kPer> q = *reinterpret_cast<const Vec<T, kPer> *>(l + at);
+        const bool there = word < count;
+        const int at = there ? word : count - 1;
+        const Word<T, kPer> q = get(at);
+        const int from = there ? skip(at) : kPer;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) v[i] = to_f32(q.v[i]);
+        for (int i = 0; i < kPer; ++i) v[i] = i >= from ? to_f32(q.v[i]) : kNone;
+    }
+    // Stores the gradients of a word.
+    __device__ void put(T *d, int word, const float (&v)[kPer]) const {
+        const int at = first(word), from = skip(word);
+        Word<T, kPer> o;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o.v[i] = from_f32<T>(v[i]);
+        if (from == 0) {
+            store_past(d + at, o);
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
-                v[i] = word < count && at + i >= 0 && at + i < A ? to_f32(l[at + i]) : kNone;
+                if (i >= from) store_past(d + at + i, o.v[i]);
         }
     }
 };
@@ -316,14 +327,71 @@ template <int kPer> __device__ inline float largest(const float (&v)[kPer]) {
     return m;
 }
 
-template <int kPer> __device__ inline uint64_t best_key(const float (&v)[kPer], int at) {
-    uint64_t k = 0;
+// Reductions over the kLanes neighbouring lanes of a row: within four lanes and by mirroring eight and
+// sixteen in one instruction each, wider through LDS.  Every lane gets the result, the same bits in
+// all: the two of a pair add the same two numbers.
+template <int kLanes, typename Op> __device__ inline uint32_t over_team(uint32_t x, Op op) {
+    auto with = [&](uint32_t y) { x = op(x, y); };
+    with(uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0xB1, 0xF, 0xF, true)));    // quad 1 0 3 2
+    with(uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x4E, 0xF, 0xF, true)));    // quad 2 3 0 1
+    if (kLanes > 4) with(uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x141, 0xF, 0xF, true)));
+    if (kLanes > 8) with(uint32_t(__builtin_amdgcn_mov_dpp(int(x), 0x140, 0xF, 0xF, true)));
+    if (kLanes > 16) with(uint32_t(__shfl_xor(int(x), 16)));
+    return x;
+}
+template <int kLanes> __device__ inline float team_max(float v) {
+    return __uint_as_float(over_team<kLanes>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+template <int kLanes> __device__ inline float team_sum(float v) {
+    return __uint_as_float(over_team<kLanes>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+
+// Rows of at most kLanes words, kLanes (4 to 32) lanes each and a word a lane.  Alternatives: the
+// largest left of all lanes, again and again; of equal ones the lowest lane and element has the
+// lowest index.
+template <typename T, int kLanes>
+__global__ void __launch_bounds__(256) team_rows_kernel(TokenArgs a) {
+    constexpr int kPer = Words<T>::kPer;
+    const int lane = threadIdx.x % kLanes;
+    const int64_t at = int64_t(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
+    const bool live = at < a.N;
+    const int64_t row = live ? at : a.N - 1;
+    const Words<T> in(a, row);
+    Given given{};
+    if (lane == 0) given = given_of(a, row, in.l);
+    float v[kPer];
+    in.load(lane, v);
+    Stat st{team_max<kLanes>(largest(v)), 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const uint64_t o = key_of(v[i], at + i);
-        k = o > k ? o : k;
+    for (int i = 0; i < kPer; ++i) add(st, v[i]);
+    st.s = team_sum<kLanes>(st.s);
+    st.w = team_sum<kLanes>(st.w);
+    const Row r = row_of(st);
+    if (lane == 0 && live) put_row(a, r, row, given);
+    if (a.top == 0) return;
+    uint32_t key[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i] = uint32_t(key_of(v[i], 0) >> 32);
+    const int shift = int(threadIdx.x & 63) / kLanes * kLanes;        // the team's first lane
+    for (int j = 0; j < a.top; ++j) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) best = max(best, key[i]);
+        const uint32_t top = over_team<kLanes>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
+        const uint64_t team = __ballot(best == top) >> shift & ((uint64_t(1) << kLanes) - 1);
+        if (lane != __ffsll(static_cast<unsigned long long>(team)) - 1) continue;
+        int which = kPer - 1;
+#pragma unroll
+        for (int i = kPer - 2; i >= 0; --i) which = key[i] == top ? i : which;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[i] = i == which ? 0 : key[i];
+        const uint32_t index = uint32_t(in.first(lane) + which);
+        if (live) put_top(a, r, row, j, top ? uint64_t(top) << 32 | uint32_t(~index) : 0);
     }
-    return k;
 }
 
 // The k-th largest of the wave's 64 numbers (0 if fewer are set): bit by bit from the top, the
@@ -421,47 +489,15 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     }
 }
 
-// Stores a word past the caches: the gradient is not read again here, and the logits, which the
-// forward pass has just read, stay (4096 x 32768 in bf16, both passes: 169 us, so 142).
-template <typename T, int n> __device__ inline void put_past(T *to, const Vec<T, n> &v) {
-    static_assert(sizeof v == 16, "one word");
-    typedef uint32_t Word __attribute__((ext_vector_type(4)));
-    Word u;
-    __builtin_memcpy(&u, &v, 16);
-    __builtin_nontemporal_store(u, reinterpret_cast<Word *>(to));
-}
-
-// The whole words of a row, and the elements before and after them, which the first 2 kPer threads
-// take one by one (head, then tail); or one part of `parts` of them: the words from..to - 1, the
-// head with the first part and the tail with the last.
-template <typename T> struct Parts {
-    static constexpr int kPer = 16 / sizeof(T);
-    const T *l;
-    int head, words, tail, from, to;
+// The words of one of `parts` parts of a row.
+template <typename T> struct Parts : Words<T> {
+    int from, to;
 
     __device__ Parts(const TokenArgs &a, int64_t row, int part = 0, int parts = 1)
-        : l(static_cast<const T *>(a.logits) + row * a.stride) {
-        head = min(a.A, int(-(reinterpret_cast<uintptr_t>(l) / sizeof(T)) % kPer));
-        words = (a.A - head) / kPer;
-        tail = a.A - head - words * kPer;
-        const int each = (words + parts - 1) / parts;
-        from = min(words, part * each);
-        to = min(words, from + each);
-        if (part > 0) head_of = 0;
-        if (part < parts - 1) tail_of = 0;
-    }
-    int head_of = 1 << 30, tail_of = 1 << 30;        // limits on the ends this part takes
-    __device__ Vec<T, kPer> word(int w) const {
-        return reinterpret_cast<const Vec<T, kPer> *>(l + head)[w];
-    }
-    __device__ int first(int w) const { return head + w * kPer; }
-    // The single element of a thread: its index, or -1.
-    __device__ int single(int tid, bool after) const {
-        if (after) {
-            const int i = tid - kPer;
-            return i >= 0 && i < min(tail, tail_of) ? head + words * kPer + i : -1;
-        }
-        return tid < min(head, head_of) ? tid : -1;
+        : Words<T>(a, row) {
+        const int each = (this->count + parts - 1) / parts;
+        from = min(this->count, part * each);
+        to = min(this->count, from + each);
     }
 };
 
@@ -490,15 +526,12 @@ __device__ void alternatives(const TokenArgs &a, const Parts<T> &in, float m, Pu
     for (int exact = 0; exact < 2; ++exact) {
         if (exact) {
             best = 0;
-            for (int after = 0; after < 2; ++after) {
-                const int i = in.single(tid, after);
-                if (i >= 0) best = max(best, key_of(to_f32(in.l[i]), i));
-            }
             for (int word = in.from + tid; word < in.to; word += kThreads) {
-                const Vec<T, kPer> q = in.word(word);
+                float v[kPer];
+                in.load(word, v);
 #pragma unroll
                 for (int i = 0; i < kPer; ++i)
-                    if (to_f32(q.v[i]) == m) best = max(best, key_of(m, in.first(word) + i));
+                    if (v[i] == m) best = max(best, key_of(m, in.first(word) + i));
             }
         }
         const uint64_t mine = exact ? kth_of_wave(best, a.top)
@@ -517,17 +550,14 @@ __device__ void alternatives(const TokenArgs &a, const Parts<T> &in, float m, Pu
             const int at = atomicAdd(&listed, 1);
             if (at < kList) list[at] = k;
         };
-        for (int after = 0; after < 2; ++after) {
-            const int i = in.single(tid, after);
-            if (i >= 0) offer(to_f32(in.l[i]), i);
-        }
         const int tasks = held * each;
         for (int t = tid; t < tasks; t += kThreads) {
             const int word = in.from + holders[t / each] + t % each * kThreads;
             if (word >= in.to) continue;
-            const Vec<T, kPer> q = in.word(word);
+            float v[kPer];
+            in.load(word, v);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) offer(to_f32(q.v[i]), in.first(word) + i);
+            for (int i = 0; i < kPer; ++i) offer(v[i], in.first(word) + i);
         }
         __syncthreads();
         const int n = listed;
@@ -548,14 +578,11 @@ __device__ void alternatives(const TokenArgs &a, const Parts<T> &in, float m, Pu
             const uint64_t k = key_of(v, i);
             if (k < last && k > next) next = k;
         };
-        for (int after = 0; after < 2; ++after) {
-            const int i = in.single(tid, after);
-            if (i >= 0) look(to_f32(in.l[i]), i);
-        }
         for (int word = in.from + tid; word < in.to; word += kThreads) {
-            const Vec<T, kPer> q = in.word(word);
+            float v[kPer];
+            in.load(word, v);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) look(to_f32(q.v[i]), in.first(word) + i);
+            for (int i = 0; i < kPer; ++i) look(v[i], in.first(word) + i);
         }
         next = wave_max(next);
         __syncthreads();
@@ -579,33 +606,41 @@ __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
     const Parts<T> in(a, row, kSplit ? blockIdx.y : 0, kSplit ? a.parts : 1);
     Given given{};
     if (!kSplit && tid == 0) given = given_of(a, row, in.l);
-    // the row's ends
-    const int before = in.single(tid, false), after = in.single(tid, true);
-    const float va = before >= 0 ? to_f32(in.l[before]) : kNone;
-    const float vb = after >= 0 ? to_f32(in.l[after]) : kNone;
-    Stat st{fmaxf(va, vb), 0.0f, 0.0f};
-    add(st, va);
-    add(st, vb);
+    Stat st{kNone, 0.0f, 0.0f};
     for (int word = in.from + tid; word < in.to; word += kWords * kThreads) {
-        Vec<T, kPer> q[kWords];
-        const bool whole = word + (kWords - 1) * kThreads < in.to;
-#pragma unroll
-        for (int j = 0; j < kWords; ++j)               // past the end: the last word again
-            q[j] = in.word(whole ? word + j * kThreads : min(word + j * kThreads, in.to - 1));
+        Word<T, kPer> q[kWords];
+        // all of this round's words are there, and none is the row's last, which may skip elements
+        const bool whole = word + (kWords - 1) * kThreads < min(in.to, in.count - 1);
         float m = st.m;
+        if (whole) {
 #pragma unroll
-        for (int j = 0; j < kWords; ++j)
-            if (whole || word + j * kThreads < in.to) {
+            for (int j = 0; j < kWords; ++j) q[j] = in.get(word + j * kThreads);
+#pragma unroll
+            for (int j = 0; j < kWords; ++j)
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) m = fmaxf(m, to_f32(q[j].v[i]));
-            }
-        if (m > st.m) raise(st, m);
+            if (m > st.m) raise(st, m);
 #pragma unroll
-        for (int j = 0; j < kWords; ++j)
-            if (whole || word + j * kThreads < in.to) {
+            for (int j = 0; j < kWords; ++j)
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) add(st, to_f32(q[j].v[i]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) q[j] = in.get(min(word + j * kThreads, in.to - 1));
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) {
+                const int at = word + j * kThreads;
+                if (at >= in.to) continue;
+                const int from = in.skip(at);
+                float v[kPer];
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) v[i] = i >= from ? to_f32(q[j].v[i]) : kNone;
+                m = largest(v);
+                if (m > st.m) raise(st, m);
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) add(st, v[i]);
             }
+        }
     }
     const float mine = st.m;
     st = join_lanes(st);
@@ -672,68 +707,43 @@ template <typename T> __global__ void __launch_bounds__(256) join_rows_kernel(To
     for (int j = m + tid; j < a.top; j += 256) put_top(a, r, row, j, 0);
 }
 
-// Gradient of rows of any length; kSame: dlogits' rows are as far into a word as the logits'.
-// blockIdx.y, and the threads, share a row's words.
-template <typename T, bool kSame>
+// Gradient of rows of any length; blockIdx.y, and the threads, share a row's words.  The gradient
+// goes past the caches: it is not read again here, and the logits, which the forward pass has just
+// read, stay (4096 x 32768 in bf16, both passes: 169 us, so 142).
+template <typename T>
 __global__ void __launch_bounds__(256) long_back_kernel(TokenArgs a) {
-    constexpr int kPer = Parts<T>::kPer;
+    constexpr int kPer = Words<T>::kPer;
     const int64_t row = blockIdx.x;
-    const Parts<T> in(a, row);
+    const Words<T> in(a, row);
     T *d = static_cast<T *>(a.dlogits) + row * a.dstride;
     const Back b = back_of(a, row);
-    if (blockIdx.y == 0) {
-        for (int after = 0; after < 2; ++after) {
-            const int i = in.single(threadIdx.x, after);
-            if (i < 0) continue;
-            float v[1] = {to_f32(in.l[i])};
-            slopes(b, i, v);
-            d[i] = from_f32<T>(v[0]);
-        }
-    }
     const int stride = int(gridDim.y) * 256;
-    for (int word = int(blockIdx.y) * 256 + threadIdx.x; word < in.words; word += stride) {
-        const Vec<T, kPer> q = in.word(word);
-        const int at = in.first(word);
+    for (int word = int(blockIdx.y) * 256 + threadIdx.x; word < in.count; word += stride) {
+        const Word<T, kPer> q = in.get(word);
         float v[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) v[i] = to_f32(q.v[i]);
-        slopes(b, at, v);
-        Vec<T, kPer> o;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) o.v[i] = from_f32<T>(v[i]);
-        if (kSame) {
-            put_past(d + at, o);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) d[at + i] = o.v[i];
-        }
+        slopes(b, in.first(word), v);
+        in.put(d, word, v);
     }
 }
 
-// The same for rows of at most kWaveRow choices, a wave each.
-template <typename T, bool kSame>
-__global__ void __launch_bounds__(256) wave_back_kernel(TokenArgs a) {
+// The same for rows of at most kWaveRow choices, kLanes lanes each.
+template <typename T, int kLanes>
+__global__ void __launch_bounds__(256) team_back_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
-    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t row = int64_t(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
     if (row >= a.N) return;
     const Words<T> in(a, row);
     T *d = static_cast<T *>(a.dlogits) + row * a.dstride;
     const Back b = back_of(a, row);
-    for (int word = threadIdx.x & 63; word < in.count; word += 64) {
+    for (int word = threadIdx.x % kLanes; word < in.count; word += kLanes) {
+        const Word<T, kPer> q = in.get(word);
         float v[kPer];
-        in.load(word, v);
-        const int at = in.first(word);
-        slopes(b, at, v);
-        Vec<T, kPer> o;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) o.v[i] = from_f32<T>(v[i]);
-        if (kSame && in.whole(word)) {
-            *reinterpret_cast<Vec<T, kPer> *>(d + at) = o;
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (at + i >= 0 && at + i < a.A) d[at + i] = o.v[i];
-        }
+        for (int i = 0; i < kPer; ++i) v[i] = to_f32(q.v[i]);
+        slopes(b, in.first(word), v);
+        in.put(d, word, v);
     }
 }
 
@@ -798,8 +808,9 @@ __global__ void __launch_bounds__(256) draw_kernel(TokenArgs a) {
 
 unsigned blocks_of(int64_t n, int64_t per) { return unsigned((n + per - 1) / per); }
 
-template <typename T> int words_of(const TokenArgs &a) {     // most words a row can take
-    return int((int64_t(a.A) + 16 / sizeof(T) - 2) / (16 / sizeof(T))) + 1;
+template <typename T> int words_of(const TokenArgs &a) {
+    constexpr int kPer = 16 / sizeof(T);
+    return (a.A + kPer - 1) / kPer;
 }
 
 // Rows one behind the other from a 16-byte border on: moved through LDS.
@@ -829,13 +840,17 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
         if (packed_rows(a, a.logits, a.stride)) return small_forward<T, true>(a, s);
         return small_forward<T, false>(a, s);
     }
-    const int lanes = blocks_of(words_of<T>(a), 64);
-    if (a.A <= kWaveRow && lanes <= 8) {
-        const dim3 g(blocks_of(a.N, 4));
-        if (lanes <= 1) hipLaunchKernelGGL((wave_rows_kernel<T, 1>), g, b, 0, s, a);
-        else if (lanes <= 2) hipLaunchKernelGGL((wave_rows_kernel<T, 2>), g, b, 0, s, a);
-        else if (lanes <= 4) hipLaunchKernelGGL((wave_rows_kernel<T, 4>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((wave_rows_kernel<T, 8>), g, b, 0, s, a);
+    if (a.A <= kWaveRow) {
+        const int words = words_of<T>(a);
+        auto rows = [&](int lanes) { return dim3(blocks_of(a.N, 256 / lanes)); };
+        if (words <= 4) hipLaunchKernelGGL((team_rows_kernel<T, 4>), rows(4), b, 0, s, a);
+        else if (words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 8>), rows(8), b, 0, s, a);
+        else if (words <= 16) hipLaunchKernelGGL((team_rows_kernel<T, 16>), rows(16), b, 0, s, a);
+        else if (words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 32>), rows(32), b, 0, s, a);
+        else if (words <= 64) hipLaunchKernelGGL((wave_rows_kernel<T, 1>), rows(64), b, 0, s, a);
+        else if (words <= 128) hipLaunchKernelGGL((wave_rows_kernel<T, 2>), rows(64), b, 0, s, a);
+        else if (words <= 256) hipLaunchKernelGGL((wave_rows_kernel<T, 4>), rows(64), b, 0, s, a);
+        else hipLaunchKernelGGL((wave_rows_kernel<T, 8>), rows(64), b, 0, s, a);
         return hipGetLastError();
     }
     const dim3 g(unsigned(a.N), unsigned(a.parts));
@@ -859,23 +874,20 @@ template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
             return small_backward<T, true>(a, s);
         return small_backward<T, false>(a, s);
     }
-    constexpr int kPer = 16 / sizeof(T);
-    const bool same = (reinterpret_cast<uintptr_t>(a.logits) -
-                       reinterpret_cast<uintptr_t>(a.dlogits)) % 16 == 0 &&
-                      (a.stride - a.dstride) % kPer == 0;
+    const int words = words_of<T>(a);
     if (a.A <= kWaveRow) {
-        const dim3 g(blocks_of(a.N, 4));
-        if (same) hipLaunchKernelGGL((wave_back_kernel<T, true>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((wave_back_kernel<T, false>), g, b, 0, s, a);
+        auto rows = [&](int lanes) { return dim3(blocks_of(a.N, 256 / lanes)); };
+        if (words <= 4) hipLaunchKernelGGL((team_back_kernel<T, 4>), rows(4), b, 0, s, a);
+        else if (words <= 8) hipLaunchKernelGGL((team_back_kernel<T, 8>), rows(8), b, 0, s, a);
+        else if (words <= 16) hipLaunchKernelGGL((team_back_kernel<T, 16>), rows(16), b, 0, s, a);
+        else if (words <= 32) hipLaunchKernelGGL((team_back_kernel<T, 32>), rows(32), b, 0, s, a);
+        else hipLaunchKernelGGL((team_back_kernel<T, 64>), rows(64), b, 0, s, a);
         return hipGetLastError();
     }
     // enough workgroups for the device where the rows are few
-    const int words = words_of<T>(a);
     const int per_row = int(std::max<int64_t>(1, std::min<int64_t>(blocks_of(words, 256),
                                                                    (2048 + a.N - 1) / a.N)));
-    const dim3 g(unsigned(a.N), unsigned(per_row));
-    if (same) hipLaunchKernelGGL((long_back_kernel<T, true>), g, b, 0, s, a);
-    else hipLaunchKernelGGL((long_back_kernel<T, false>), g, b, 0, s, a);
+    hipLaunchKernelGGL((long_back_kernel<T>), dim3(unsigned(a.N), unsigned(per_row)), b, 0, s, a);
     return hipGetLastError();
 }
 

@@ -1,5 +1,5 @@
 // Element types of the learner's operators (k_scan.hip, k_tokens.hip): storage, conversion to
-// and from 32-bit arithmetic, and vectors of V elements moved as one word.
+// and from 32-bit arithmetic, and groups of V elements moved as one word.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -25,6 +25,30 @@ template <> __device__ inline bf16_t from_f32<bf16_t>(float v) {
     return r;
 }
 
-template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
+// V neighbouring elements.  Global memory takes an access of up to 16 bytes at any address, so one
+// of V elements needs no more alignment than its element's.
+template <typename T, int V> struct Word { T v[V]; };
+typedef uint64_t Any2 __attribute__((ext_vector_type(2)));
+template <int kBytes> struct Bits;
+template <> struct Bits<1> { typedef uint8_t type; };
+template <> struct Bits<2> { typedef uint16_t type __attribute__((aligned(1))); };
+template <> struct Bits<4> { typedef uint32_t type __attribute__((aligned(1))); };
+template <> struct Bits<8> { typedef uint64_t type __attribute__((aligned(1))); };
+template <> struct Bits<16> { typedef Any2 type __attribute__((aligned(1))); };
+
+template <typename E> __device__ inline E load_any(const void *p) {
+    const typename Bits<sizeof(E)>::type u =
+        *static_cast<const typename Bits<sizeof(E)>::type *>(p);
+    E e;
+    __builtin_memcpy(&e, &u, sizeof e);
+    return e;
+}
+// Written past the caches.
+template <typename E> __device__ inline void store_past(void *p, const E &e) {
+    typedef typename Bits<sizeof(E)>::type U;
+    U u;
+    __builtin_memcpy(&u, &e, sizeof u);
+    __builtin_nontemporal_store(u, static_cast<U *>(p));
+}
 
 }  // namespace av
