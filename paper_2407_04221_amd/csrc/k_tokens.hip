@@ -749,58 +749,98 @@ __global__ void __launch_bounds__(256) team_back_kernel(TokenArgs a) {
 
 // ---- drawing ----
 
-// In 64 bits, so that where the sum passes u is a property of the logits and not of the order or
-// the type of the sum.  Rows of up to kA = 4 kLanes choices, four neighbouring ones a lane.
-template <typename T, int kLanes>
+// Sums of the lanes up to and with this one, of a row's kLanes; and the row's total.
+template <int kLanes, typename F> __device__ inline F upto_lane(F x, int lane) {
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) {
+        const F o = __shfl_up(x, d, kLanes);
+        if (lane >= d) x += o;
+    }
+    return x;
+}
+
+constexpr int kNoChoice = 1 << 20;
+
+// Rows of up to kEach kLanes choices, kEach neighbouring ones a lane.  Where the sum passes u is a
+// property of the logits in 64 bits, but is found in 32 unless it is close.  With e_i = 2^t_i,
+// t_i <= 0, a weight is off by at most (1 + |t_i| ln 2) 2^-23 of itself and sum p_i |t_i| <= log2 A <= 8,
+// so that a running sum, with its fourteen additions, and u times the total are off by less than
+// 16 x 2^-23 of the total: a sum further than 2^-17 of the total from u x total is on the side it
+// seems to be.  The rows of a wave that holds a closer one (a row of 256 choices in some 250 does,
+// one of 5 in 13000) are drawn again in 64 bits (26421 rows of 135 choices: 11 us, all in 64 bits 22).
+template <typename T, int kLanes, int kEach>
 __global__ void __launch_bounds__(256) draw_kernel(TokenArgs a) {
     const int lane = threadIdx.x % kLanes;
     const int64_t row = int64_t(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
     const bool live = row < a.N;
     const T *l = static_cast<const T *>(a.logits) + (live ? row : a.N - 1) * a.stride;
-    float v[4];
+    const float u = a.uniform[live ? row : a.N - 1];
+    float v[kEach];
+    if (lane * kEach + kEach <= a.A) {
+        const Word<T, kEach> q = load_any<Word<T, kEach>>(l + lane * kEach);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = lane * 4 + i < a.A ? to_f32(l[lane * 4 + i]) : kNone;
+        for (int i = 0; i < kEach; ++i) v[i] = to_f32(q.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            v[i] = lane * kEach + i < a.A ? to_f32(l[lane * kEach + i]) : kNone;
+    }
     float m = largest(v);
 #pragma unroll
     for (int d = kLanes / 2; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, kLanes));
-    double e[4], sum = 0.0;
+    float e[kEach], sum = 0.0f;
+    int alive = -1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        e[i] = v[i] == kNone ? 0.0 : exp(double(v[i]) - double(m));
+    for (int i = 0; i < kEach; ++i) {
+        e[i] = v[i] == kNone ? 0.0f : exp2_of((v[i] - m) * kLog2e);
         sum += e[i];
         e[i] = sum;                                   // up to and with choice i
+        if (v[i] > kNone) alive = lane * kEach + i;
     }
-    double upto = sum;                                // of the lanes up to and with this one
+    const float upto = upto_lane<kLanes>(sum, lane), total = __shfl(upto, kLanes - 1, kLanes);
+    float before = __shfl_up(upto, 1, kLanes);
+    if (lane == 0) before = 0.0f;
+    const float aim = u * total;
+    int pick = kNoChoice;
+    bool close = false;
 #pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) {
-        const double o = __shfl_up(upto, d, kLanes);
-        if (lane >= d) upto += o;
+    for (int i = kEach - 1; i >= 0; --i) {
+        if (!(v[i] > kNone)) continue;
+        const float over = before + e[i] - aim;
+        if (over > 0.0f) pick = lane * kEach + i;
+        close |= fabsf(over) <= total * 0x1p-17f;
     }
-    const double total = __shfl(upto, kLanes - 1, kLanes);
-    double before = __shfl_up(upto, 1, kLanes);
-    if (lane == 0) before = 0.0;
-    const double aim = live ? double(a.uniform[row]) * total : 0.0;
-    int pick = 1 << 20, alive = -1;
+    if (__any(close)) {
+        double w[kEach], s = 0.0;
 #pragma unroll
-    for (int i = 3; i >= 0; --i) {
-        if (v[i] > kNone && alive < 0) alive = lane * 4 + i;
-        if (v[i] > kNone && before + e[i] > aim) pick = lane * 4 + i;
+        for (int i = 0; i < kEach; ++i) {
+            s += v[i] == kNone ? 0.0 : exp(double(v[i]) - double(m));
+            w[i] = s;
+        }
+        const double to = upto_lane<kLanes>(s, lane);
+        const double goal = double(u) * __shfl(to, kLanes - 1, kLanes);
+        double from = __shfl_up(to, 1, kLanes);
+        if (lane == 0) from = 0.0;
+        pick = kNoChoice;
+#pragma unroll
+        for (int i = kEach - 1; i >= 0; --i)
+            if (v[i] > kNone && from + w[i] > goal) pick = lane * kEach + i;
     }
 #pragma unroll
     for (int d = kLanes / 2; d > 0; d >>= 1) {
         pick = min(pick, __shfl_xor(pick, d, kLanes));
         alive = max(alive, __shfl_xor(alive, d, kLanes));
     }
-    if (pick == 1 << 20) pick = alive;
+    if (pick == kNoChoice) pick = alive;
     if (!live || lane != 0) return;
     float logp = kNone;
-    if (!(total < double(__builtin_inff()))) {        // a NaN, or a +inf
+    if (!(total < __builtin_inff())) {                // a NaN, or a +inf
         pick = 0;
         logp = __builtin_nanf("");
     } else if (pick < 0) {
         pick = 0;
     } else {
-        logp = float(double(to_f32(l[pick])) - double(m) - log(total));
+        logp = fmaf(-kLn2, log2f(total), to_f32(l[pick]) - m);
     }
     a.actions[row] = uint8_t(pick);
     if (a.logp) a.logp[row] = logp;
@@ -893,9 +933,10 @@ template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
 
 template <typename T> hipError_t draw(const TokenArgs &a, hipStream_t s) {
     const dim3 b(256);
-    if (a.A <= 8) hipLaunchKernelGGL((draw_kernel<T, 2>), dim3(blocks_of(a.N, 128)), b, 0, s, a);
-    else if (a.A <= 64) hipLaunchKernelGGL((draw_kernel<T, 16>), dim3(blocks_of(a.N, 16)), b, 0, s, a);
-    else hipLaunchKernelGGL((draw_kernel<T, 64>), dim3(blocks_of(a.N, 4)), b, 0, s, a);
+    if (a.A <= 8) hipLaunchKernelGGL((draw_kernel<T, 2, 4>), dim3(blocks_of(a.N, 128)), b, 0, s, a);
+    else if (a.A <= 64) hipLaunchKernelGGL((draw_kernel<T, 8, 8>), dim3(blocks_of(a.N, 32)), b, 0, s, a);
+    else if (a.A <= 128) hipLaunchKernelGGL((draw_kernel<T, 16, 8>), dim3(blocks_of(a.N, 16)), b, 0, s, a);
+    else hipLaunchKernelGGL((draw_kernel<T, 32, 8>), dim3(blocks_of(a.N, 8)), b, 0, s, a);
     return hipGetLastError();
 }
 

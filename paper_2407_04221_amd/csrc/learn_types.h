@@ -29,12 +29,14 @@ template <> __device__ inline bf16_t from_f32<bf16_t>(float v) {
 // of V elements needs no more alignment than its element's.
 template <typename T, int V> struct Word { T v[V]; };
 typedef uint64_t Any2 __attribute__((ext_vector_type(2)));
+typedef uint64_t Any4 __attribute__((ext_vector_type(4)));
 template <int kBytes> struct Bits;
 template <> struct Bits<1> { typedef uint8_t type; };
 template <> struct Bits<2> { typedef uint16_t type __attribute__((aligned(1))); };
 template <> struct Bits<4> { typedef uint32_t type __attribute__((aligned(1))); };
 template <> struct Bits<8> { typedef uint64_t type __attribute__((aligned(1))); };
 template <> struct Bits<16> { typedef Any2 type __attribute__((aligned(1))); };
+template <> struct Bits<32> { typedef Any4 type __attribute__((aligned(1))); };    // two accesses
 
 template <typename E> __device__ inline E load_any(const void *p) {
     const typename Bits<sizeof(E)>::type u =

@@ -253,8 +253,7 @@ def test_parts_on_request():
 
 
 def test_one_row_for_all():
-    """A row stride of 0.  (The rows of a copy start at other places of a 16-byte word, so their sums
-    are taken in another order: both are held to the bound, not to each other's bits.)"""
+    """A row stride of 0."""
     row = torch.randn((1, 50), device="cuda")
     logits, ids = row.expand(20, 50), torch.arange(20, device="cuda")
     a, b = torch.empty(20, device="cuda"), torch.empty(20, device="cuda")
@@ -268,7 +267,7 @@ def test_one_row_for_all():
                                  torch.empty((1, 50), device="cuda").expand(20, 50))
 
 
-@pytest.mark.parametrize("A", [1, 2, 5, 8, 9, 17, 64, 65, 255, 256])
+@pytest.mark.parametrize("A", [1, 2, 5, 8, 9, 17, 64, 65, 128, 129, 255, 256])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_draw(A, dtype):
     for N in (1, 131, 1000):
@@ -285,8 +284,12 @@ def test_draw(A, dtype):
         av.av_draw_actions(logits, torch.from_numpy(u).cuda(), actions, logp)
         want, want_logp = ref.draw(host(logits), u)
         assert np.array_equal(actions.cpu().numpy(), want)
-        # rounded once from 64 bits
-        ref.check(host(logp), (want_logp, ref.U * np.abs(np.nan_to_num(want_logp)) + 1e-12), "logp")
+        # the sum of weights in 32 bits: each is off by (1 + |t| ln 2) 2 U of itself with the mean of
+        # |t| at most log2 A, fourteen additions and the logarithm by U each: 2 (1 + 0.7 log2 A) + 16
+        # of U, and the two subtractions by U of what they give and of the logits' distance
+        size = np.abs(np.nan_to_num(want_logp, neginf=0.0))
+        bound = ref.U * (18.0 + 1.4 * np.log2(max(A, 2)) + 3.0 * size + 2.0 * np.log(A))
+        ref.check(host(logp), (want_logp, bound), "logp")
         again = torch.empty_like(actions)
         av.av_draw_actions(logits, torch.from_numpy(u).cuda(), again)
         assert torch.equal(again, actions)
@@ -339,6 +342,24 @@ def test_draw_follows_the_distribution():
     av.av_draw_actions(logits, u, actions)
     count = np.bincount(actions.cpu().numpy(), minlength=5)
     assert (np.abs(count - p * N) <= 2).all() and count[1] == 0
+
+
+def test_draw_close_to_a_border():
+    """Numbers at and next to the borders between choices, where 32 bits do not tell the side."""
+    for A in (5, 64, 200):
+        N = 4 * A
+        logits = torch.zeros((N, A), device="cuda")
+        i = np.repeat(np.arange(A), 4)
+        u = (i / A).astype(np.float32)
+        u[1::4] = np.nextafter(u[1::4], 2.0, dtype=np.float32)
+        u[2::4] = np.nextafter(u[2::4], -1.0, dtype=np.float32)
+        u[3::4] += np.float32(2.0 ** -21)
+        u = np.clip(u, 0.0, np.float32(1.0 - 2.0 ** -24))
+        actions = torch.empty(N, dtype=torch.uint8, device="cuda")
+        av.av_draw_actions(logits, torch.from_numpy(u).cuda(), actions)
+        # equal weights: the first i with (i + 1) > u A, u and A exact in 64 bits
+        want = np.minimum(np.floor(u.astype(np.float64) * A), A - 1)
+        assert np.array_equal(actions.cpu().numpy(), want)
 
 
 def test_binding_refuses():
