@@ -473,12 +473,14 @@ av_status av_scan_workspace(const av_scan_config *cfg, int32_t backward, size_t 
  *             processed one (T = 0: h0).  They may be the same buffer.
  *   y         device, dtype; may be x itself (the same pointer and strides)
  * Products of gates are formed over spans of steps: gates are decays, |a| <= 1 (larger ones work
- * while their product over any span is finite in 32 bits).  A state that is not finite leaves every
+ * while their product over any span is finite in 32 bits; one below the smallest number in 32 bits
+ * counts as 0).  A state that is not finite leaves every
  * later output of its column not finite until the next cut.
  * workspace: av_scan_workspace bytes or more, 16-byte aligned, not shared by calls that may
  * overlap (two graphs, two streams); NULL where that is 0.  AV_EINVAL, before any device work, for
  * NULL pointers, sizes or types out of range, an output stride that makes its elements
- * overlap, a workspace too small. */
+ * overlap, a workspace too small, and for more than 2^16 steps of rows so far apart that those of
+ * 256 neighbouring columns do not lie within 2^32 bytes (call with fewer rows at a time). */
 av_status av_scan(const av_scan_config *cfg, const void *x, const void *gate, const uint8_t *cut,
                   const float *h0, void *y, float *last, void *workspace,
                   size_t workspace_bytes);
@@ -519,7 +521,8 @@ av_status av_log_probs_workspace(const av_tokens_config *cfg, size_t *bytes);
  *             its logp is 0 and it passes no gradient to the logits.
  *   logp      device float [N] or NULL
  *   entropy   device float [N] or NULL, in nats
- *   stats     device float [N][2] or NULL: the row's normaliser as av_log_probs_backward takes it
+ *   stats     device float [N][2], 8-byte aligned, or NULL: the row's normaliser as
+ *             av_log_probs_backward takes it
  *   top_logp, top_ids   device float / int32 [N][top], log-probability falling, of equal ones
  *             the lowest index first; with top = 0 not used, else neither may be NULL.
  * A logit of -infinity is a masked choice: probability 0, no part in entropy or alternatives

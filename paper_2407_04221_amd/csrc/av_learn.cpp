@@ -57,6 +57,9 @@ size_t size_of(int dtype) { return dtype == AV_F32 ? 4 : 2; }
 
 constexpr int64_t kBig = int64_t(1) << 31, kMostSteps = int64_t(1) << 30;
 constexpr int64_t kMostColumns = int64_t(1) << 28;
+// Rows too far apart for a wave's addressing take their steps one after another, at a microsecond
+// each where the rows are few: this many end in a tenth of a second.
+constexpr int64_t kMostFar = int64_t(1) << 16;
 
 av_status check_scan(const av_scan_config *c) {
     if (!c) return bad("cfg is NULL");
@@ -165,6 +168,10 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     bool far = false;
     for (const Place *a : {&px, &pg, &py, &pdy, &po, &pdg, &pc})
         if (a->p) far = far || span * a->row + width >= (int64_t(1) << 32) / int64_t(size);
+    if (far && c.steps > kMostFar)
+        return bad("%lld steps of rows too far apart: more than %lld are taken only where %lld rows "
+                   "lie within 2^32 bytes",
+                   (long long)c.steps, (long long)kMostFar, (long long)span);
     const ScanPlan plan = scan_plan(c.steps, rows, width, c.dtype, far);
     const ScanSpace space = scan_space(plan, c.rows * c.width, c.width, back && col);
     if (some) {

@@ -83,6 +83,21 @@ def test_scan_workspace(lib):
     assert av.av_scan_workspace(1 << 16, 2, 8) > 0 == av.av_scan_workspace(4, 2, 8)
 
 
+def test_many_steps_of_far_rows(lib):
+    """Rows past a wave's 32-bit distances take their steps one by one: not too many of them."""
+    apart = dict(steps=(1 << 16) + 1, rows=3, width=4, x_row=1 << 29, x_step=4, y_step=12, y_row=4,
+                 gate_per_value=1)
+    n = ctypes.c_size_t(0)
+    assert lib.av_scan_workspace(scan_config(**apart), 0, ctypes.byref(n)) == av.AV_OK
+    assert lib.av_scan(scan_config(**apart), P, P, None, None, P, None, P, n.value) == av.AV_EINVAL
+    assert "apart" in av.av_last_error()
+    far = dict(apart, x_row=4, x_step=12, dx_step=12, dx_row=4, dy_step=4, dy_row=1 << 29)
+    assert lib.av_scan_workspace(scan_config(**far), 1, ctypes.byref(n)) == av.AV_OK
+    assert lib.av_scan_backward(scan_config(**far), P, P, None, None, P, P, None, P, P, None, P,
+                                n.value) == av.AV_EINVAL
+    assert "apart" in av.av_last_error()
+
+
 def tokens_config(**kw):
     c = av.av_tokens_config()
     base = dict(rows=3, choices=5, row_stride=5, drow_stride=5)
