@@ -227,6 +227,29 @@ def test_in_place_and_state_in_place():
         assert torch.equal(d, dx) and torch.equal(g, dgate)
 
 
+@pytest.mark.parametrize("T,B,D", [(5, 300, 325), (12, 420, 325), (1000, 3, 325), (700, 1, 9)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_in_place_of_odd_widths(T, B, D, dtype):
+    """Words of columns that share some with the lane before, over what that lane writes."""
+    r = np.random.default_rng(3)
+    x, _ = make((T, B, D), dtype, r)
+    gate, _ = make((T, B, D), dtype, r)
+    dy, _ = make((T, B, D), dtype, r)
+    cut = (torch.rand((T, B), device="cuda") < 0.1).to(torch.uint8)
+    h = torch.randn((B, D), device="cuda")
+    how = dict(cut=cut, form="gated")
+    y, last, dx, dgate = (torch.empty_like(t) for t in (x, h, x, x))
+    dh = torch.empty_like(h)
+    av.av_scan(x, gate, y, h0=h, last=last, **how)
+    av.av_scan_backward(x, gate, y, dy, dx, dgate, h0=h, dlast=last, dh0=dh, **how)
+    z, state, d, g = x.clone(), h.clone(), dy.clone(), gate.clone()
+    av.av_scan(z, gate, z, h0=state, last=state, **how)
+    assert torch.equal(z, y) and torch.equal(state, last)
+    dstate = torch.empty_like(h)
+    av.av_scan_backward(x, g, y, d, d, g, h0=h, dlast=last, dh0=dstate, **how)
+    assert torch.equal(d, dx) and torch.equal(g, dgate) and torch.equal(dstate, dh)
+
+
 def test_broadcast_inputs():
     """Strides of 0: the gradient of a sum, one gate for all steps."""
     T, B, D = 40, 3, 8

@@ -252,6 +252,22 @@ def test_parts_on_request():
         assert torch.equal(same, d[4])
 
 
+@pytest.mark.parametrize("N,A", [(700, 5), (700, 7), (300, 131), (20, 2043), (40, 9001), (1, 70003)])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_gradient_over_the_logits(N, A, dtype):
+    """dlogits in the logits' own place, rows' last words sharing elements with the word before."""
+    logits, r = some(N, A, dtype, seed=8, pad=1, masked=0.05)
+    ids = torch.from_numpy(r.integers(0, A, size=N)).cuda()
+    f = dict(dtype=torch.float32, device="cuda")
+    logp, ent, stats = torch.empty(N, **f), torch.empty(N, **f), torch.empty((N, 2), **f)
+    av.av_log_probs(logits, ids, logp, ent, stats)
+    g, gh = torch.randn(N, **f), torch.randn(N, **f)
+    d = rows_of(N, A, dtype, 1, 0)
+    av.av_log_probs_backward(logits, ids, stats, ent, g, gh, d)
+    av.av_log_probs_backward(logits, ids, stats, ent, g, gh, logits)
+    assert torch.equal(d, logits)
+
+
 def test_one_row_for_all():
     """A row stride of 0."""
     row = torch.randn((1, 50), device="cuda")
