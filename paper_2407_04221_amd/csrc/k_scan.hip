@@ -614,7 +614,10 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 //   (65536 x 2 x 320 in f16: 188 us both ways, with the longest 219).
 //   Waves: eight, or sixteen where there is at most one uncut workgroup a compute unit, which has to
 //   hide its own latency (1000 x 16384 in f32: 26.3 us, with eight 27.7; but 300 x 500 x 33, some
-//   units with two workgroups: 22.1 with sixteen, 18.4 with eight).
+//   units with two workgroups: 22.1 with sixteen, 18.4 with eight).  No more of them than share an
+//   uncut recurrence's tiles evenly (300 x 16384 in f32: 14.4 us, so 13.5; 140 x 500 x 40: 11.6, so
+//   11.0), but with words, where memory is the bound, only if that drops more than a quarter (40 x
+//   1024 x 256 in f32: 27.5 us, so 23.9; but 80 x 8192 x 64 in f16, a quarter less: 58.4, so 59.3).
 ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far) {
     ScanPlan plan{};
     plan.chunks = 1;
@@ -633,6 +636,11 @@ ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far) {
     const int64_t K = steps_of(plan.vec), groups = scan_groups(scan_places(B, D, plan.vec));
     plan.waves = int(std::min<int64_t>(cut || groups > kFill / 2 ? 8 : waves_of(plan.vec),
                                        (T + K - 1) / K));
+    if (!cut) {
+        const int64_t shares = (T + K - 1) / K, tiles = (shares + plan.waves - 1) / plan.waves;
+        const int even = int((shares + tiles - 1) / tiles);
+        if (plan.vec == 1 || even * 4 < plan.waves * 3) plan.waves = even;
+    }
     if (cut) {
         const int64_t tile = plan.waves * K, tiles = (T + tile - 1) / tile;
         const int64_t want = std::min((kFill + groups - 1) / groups, tiles);
