@@ -22,7 +22,12 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 constexpr int kThreadRow = 16;      // longest row of one thread
-constexpr int kWaveRow = 2048;      // longest row of one wave
+// Longest row of one wave: 64 numbers a lane.  (20000 x 3000: in bf16 44 us as workgroups, so 31, in f32
+// 50 and 46; of 4096 in f32 59 and 61; of 8192 in bf16 73 and 127.)
+constexpr int kWaveRow = 4096;
+// Longest row of one wave in the gradient, in 16-byte words: longer ones give each thread of a workgroup
+// a word (50000 x 2040 in f32: 205 us as waves, so 139; x 1600 in bf16: 60 and 70).
+constexpr int kTeamBack = 256;
 constexpr float kNone = -__builtin_inff();
 
 __device__ inline int64_t id_of(const TokenArgs &a, int64_t row) {
@@ -728,7 +733,7 @@ __global__ void __launch_bounds__(256) long_back_kernel(TokenArgs a) {
     }
 }
 
-// The same for rows of at most kWaveRow choices, kLanes lanes each.
+// The same for rows of at most kTeamBack words, kLanes lanes each.
 template <typename T, int kLanes>
 __global__ void __launch_bounds__(256) team_back_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
@@ -890,7 +895,12 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
         else if (words <= 64) hipLaunchKernelGGL((wave_rows_kernel<T, 1>), rows(64), b, 0, s, a);
         else if (words <= 128) hipLaunchKernelGGL((wave_rows_kernel<T, 2>), rows(64), b, 0, s, a);
         else if (words <= 256) hipLaunchKernelGGL((wave_rows_kernel<T, 4>), rows(64), b, 0, s, a);
-        else hipLaunchKernelGGL((wave_rows_kernel<T, 8>), rows(64), b, 0, s, a);
+        else if (words <= 384) hipLaunchKernelGGL((wave_rows_kernel<T, 6>), rows(64), b, 0, s, a);
+        else if (words <= 512) hipLaunchKernelGGL((wave_rows_kernel<T, 8>), rows(64), b, 0, s, a);
+        else if constexpr (sizeof(T) == 4) {
+            if (words <= 768) hipLaunchKernelGGL((wave_rows_kernel<T, 12>), rows(64), b, 0, s, a);
+            else hipLaunchKernelGGL((wave_rows_kernel<T, 16>), rows(64), b, 0, s, a);
+        }
         return hipGetLastError();
     }
     const dim3 g(unsigned(a.N), unsigned(a.parts));
@@ -915,7 +925,7 @@ template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
         return small_backward<T, false>(a, s);
     }
     const int words = words_of<T>(a);
-    if (a.A <= kWaveRow) {
+    if (words <= kTeamBack) {
         auto rows = [&](int lanes) { return dim3(blocks_of(a.N, 256 / lanes)); };
         if (words <= 4) hipLaunchKernelGGL((team_back_kernel<T, 4>), rows(4), b, 0, s, a);
         else if (words <= 8) hipLaunchKernelGGL((team_back_kernel<T, 8>), rows(8), b, 0, s, a);

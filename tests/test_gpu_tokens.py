@@ -67,6 +67,17 @@ def test_sizes(A, dtype):
     compare(logits, r.integers(-1, A + 1, size=7), dtype, top=min(A, 6))
 
 
+@pytest.mark.parametrize("A", [2100, 3001, 3100, 4095, 4096, 4097])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_longest_rows_of_a_wave(A, dtype):
+    logits, r = some(6, A, dtype, seed=A, masked=0.1)
+    ids = r.integers(0, A, size=6)
+    compare(logits, ids, dtype, top=9)
+    logits[2] = 0.5                             # all equal: too many for a list of candidates
+    logits[3, 5:] = -np.inf                     # fewer than the alternatives
+    compare(logits, ids, dtype, top=9)
+
+
 @pytest.mark.parametrize("N,A", [(1, 5), (255, 5), (256, 5), (257, 5), (1000, 3), (5, 100), (1, 70000),
                                  (600, 2500), (511, 4100), (3000, 40)])
 def test_rows(N, A):
