@@ -355,9 +355,34 @@ template <int kLanes> __device__ inline float team_sum(float v) {
     }));
 }
 
-// Rows of at most kLanes words, kLanes (4 to 32) lanes each and a word a lane.  Alternatives: the
-// largest left of all lanes, again and again; of equal ones the lowest lane and element has the
-// lowest index.
+// The alternatives of a row that kLanes lanes hold, one word each: the largest left of all lanes, again
+// and again; of equal ones the lowest lane and element has the lowest index.
+template <int kLanes, int kPer, typename Index>
+__device__ inline void largest_first(const TokenArgs &a, const Row &r, int64_t row, bool live, int lane,
+                                     const float (&v)[kPer], Index index) {
+    uint32_t key[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) key[i] = uint32_t(key_of(v[i], 0) >> 32);
+    const int shift = int(threadIdx.x & 63) / kLanes * kLanes;        // the team's first lane
+    for (int j = 0; j < a.top; ++j) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) best = max(best, key[i]);
+        uint32_t top;
+        if constexpr (kLanes == 64) top = wave_max(best);
+        else top = over_team<kLanes>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
+        const uint64_t team = __ballot(best == top) >> shift & (~uint64_t(0) >> (64 - kLanes));
+        if (lane != __ffsll(static_cast<unsigned long long>(team)) - 1) continue;
+        int which = kPer - 1;
+#pragma unroll
+        for (int i = kPer - 2; i >= 0; --i) which = key[i] == top ? i : which;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[i] = i == which ? 0 : key[i];
+        if (live) put_top(a, r, row, j, top ? uint64_t(top) << 32 | uint32_t(~index(which)) : 0);
+    }
+}
+
+// Rows of at most kLanes words, kLanes (4 to 32) lanes each and a word a lane.
 template <typename T, int kLanes>
 __global__ void __launch_bounds__(256) team_rows_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
@@ -378,25 +403,7 @@ __global__ void __launch_bounds__(256) team_rows_kernel(TokenArgs a) {
     const Row r = row_of(st);
     if (lane == 0 && live) put_row(a, r, row, given);
     if (a.top == 0) return;
-    uint32_t key[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) key[i] = uint32_t(key_of(v[i], 0) >> 32);
-    const int shift = int(threadIdx.x & 63) / kLanes * kLanes;        // the team's first lane
-    for (int j = 0; j < a.top; ++j) {
-        uint32_t best = key[0];
-#pragma unroll
-        for (int i = 1; i < kPer; ++i) best = max(best, key[i]);
-        const uint32_t top = over_team<kLanes>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
-        const uint64_t team = __ballot(best == top) >> shift & ((uint64_t(1) << kLanes) - 1);
-        if (lane != __ffsll(static_cast<unsigned long long>(team)) - 1) continue;
-        int which = kPer - 1;
-#pragma unroll
-        for (int i = kPer - 2; i >= 0; --i) which = key[i] == top ? i : which;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) key[i] = i == which ? 0 : key[i];
-        const uint32_t index = uint32_t(in.first(lane) + which);
-        if (live) put_top(a, r, row, j, top ? uint64_t(top) << 32 | uint32_t(~index) : 0);
-    }
+    largest_first<kLanes>(a, r, row, live, lane, v, [&](int i) { return in.first(lane) + i; });
 }
 
 // The k-th largest of the wave's 64 numbers (0 if fewer are set): bit by bit from the top, the
@@ -423,7 +430,11 @@ constexpr int kWaveList = 256;       // candidates for the alternatives of a wav
 // One wave per row of at most kWaveRow choices, held in registers.  Alternatives: no one is smaller
 // than the k-th largest of the lanes' maxima; the elements that reach it are listed in LDS, and a
 // listed key's place is the number of larger ones.  Where they are too many (equal elements, or few
-// choices left), the largest key below the last is taken again and again.
+// choices left), the largest key below the last is taken again and again.  The bound costs much the
+// same for any number; a few of a lane's single word are found sooner one after another (20000 x 300
+// in bf16: 4 alternatives 16.2 us, with the bound 17.2; 6 of them 19.8 and 17.7), and so is one of a few
+// words (20000 x 1000 in bf16: 14.0, with the bound 20.0; of eight words 66.8 and 64.8).
+constexpr int kFew = 4, kFewWords = 4;
 template <typename T, int kWords>
 __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
@@ -450,6 +461,20 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     const Row r = row_of(st);
     if (lane == 0) put_row(a, r, row, given);
     if (a.top == 0) return;
+    if (kWords == 1 && a.top <= kFew) {
+        largest_first<64>(a, r, row, true, lane, v[0], [&](int i) { return in.first(lane) + i; });
+        return;
+    }
+    if (kWords <= kFewWords && a.top == 1) {
+        int at = 0;
+#pragma unroll
+        for (int j = kWords - 1; j >= 0; --j)
+#pragma unroll
+            for (int i = kPer - 1; i >= 0; --i) at = v[j][i] == m ? in.first(j * 64 + lane) + i : at;
+        const uint64_t best = wave_max(key_of(m, at));
+        if (lane == 0) put_top(a, r, row, 0, best);
+        return;
+    }
     unsigned long long *list = lists[threadIdx.x >> 6];
     const uint64_t bound = uint64_t(kth_of_wave(uint32_t(key_of(m, 0) >> 32), a.top)) << 32;
     const float least = bound == 0 ? -__FLT_MAX__ : key_logit(bound);

@@ -67,6 +67,21 @@ def test_sizes(A, dtype):
     compare(logits, r.integers(-1, A + 1, size=7), dtype, top=min(A, 6))
 
 
+@pytest.mark.parametrize("A", [140, 300, 1000, 2001])
+@pytest.mark.parametrize("top", [1, 3, 4, 5])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_alternatives(A, top, dtype):
+    """Equal logits in several lanes and words, fewer choices than alternatives, none at all."""
+    logits, r = some(9, A, dtype, seed=A, masked=0.1)
+    logits[1] = 0.25
+    logits[2] = torch.where(torch.arange(A, device="cuda") % 37 == 5, 1.5, -2.0).to(logits.dtype)
+    logits[3, :] = -np.inf
+    logits[3, A - 1] = -7.0
+    logits[4, :] = -np.inf
+    logits[5] = torch.where(torch.arange(A, device="cuda") % 2 == 0, 0.0, -0.0).to(logits.dtype)
+    compare(logits, r.integers(0, A, size=9), dtype, top=top)
+
+
 @pytest.mark.parametrize("A", [2100, 3001, 3100, 4095, 4096, 4097])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_longest_rows_of_a_wave(A, dtype):
