@@ -626,7 +626,9 @@ __device__ void alternatives(const TokenArgs &a, const Parts<T> &in, float m, Pu
 
 // One workgroup per row of any length, or, kSplit, per part of it (blockIdx.y), whose sums and
 // alternatives go to the workspace.  A thread has kWords 16-byte words on their way at once; the
-// largest of their elements is found first, so that the sums are rescaled at most once for all.
+// largest of their elements is found first, so that the sums are rescaled at most once for all.  Four
+// words, or eight for many long rows (2500 x 60001 in f32: 122 us, with four 129; but 777 x 50021 in
+// f16 31 and 26.6, and 4096 x 9000 in bf16, which have no round of eight, 21.6 and 18.1).
 template <typename T, int kThreads, int kWords, bool kSplit>
 __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
     constexpr int kPer = Parts<T>::kPer, kWaves = kThreads / 64;
@@ -910,8 +912,8 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
         if (packed_rows(a, a.logits, a.stride)) return small_forward<T, true>(a, s);
         return small_forward<T, false>(a, s);
     }
+    const int words = words_of<T>(a);
     if (a.A <= kWaveRow) {
-        const int words = words_of<T>(a);
         auto rows = [&](int lanes) { return dim3(blocks_of(a.N, 256 / lanes)); };
         if (words <= 4) hipLaunchKernelGGL((team_rows_kernel<T, 4>), rows(4), b, 0, s, a);
         else if (words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 8>), rows(8), b, 0, s, a);
@@ -932,6 +934,8 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
     if (a.parts > 1) {
         hipLaunchKernelGGL((long_rows_kernel<T, 256, 4, true>), g, b, 0, s, a);
         hipLaunchKernelGGL((join_rows_kernel<T>), dim3(unsigned(a.N)), b, 0, s, a);
+    } else if (a.N >= 2048 && words >= 4096) {
+        hipLaunchKernelGGL((long_rows_kernel<T, 256, 8, false>), g, b, 0, s, a);
     } else if (a.N >= 2048) {
         hipLaunchKernelGGL((long_rows_kernel<T, 256, 4, false>), g, b, 0, s, a);
     } else if (a.N >= 512) {

@@ -101,6 +101,30 @@ def test_rows(N, A):
         compare(logits, r.integers(0, A, size=N), dtype, top=3)
 
 
+@pytest.mark.parametrize("A,dtype", [(16387, "f32"), (40003, "f16"), (32768, "bf16")])
+def test_many_long_rows(A, dtype):
+    """2100 rows, the first seven compared, the others the same again."""
+    few, r = some(7, A, dtype, seed=3, masked=0.1)
+    few[2, : A // 2] = -np.inf
+    few[3] = 2.0
+    ids = r.integers(0, A, size=7)
+    logits = few.repeat(300, 1)
+    N = len(logits)
+    f = dict(dtype=torch.float32, device="cuda")
+    logp, ent, stats = torch.empty(N, **f), torch.empty(N, **f), torch.empty((N, 2), **f)
+    tl, ti = torch.empty((N, 4), **f), torch.empty((N, 4), dtype=torch.int32, device="cuda")
+    wide = torch.from_numpy(ids).cuda().repeat(300)
+    av.av_log_probs(logits, wide, logp, ent, stats, tl, ti)
+    assert torch.equal(ti.view(300, 7, 4), ti[:7].expand(300, 7, 4))
+    assert torch.equal(logp.view(300, 7), logp[:7].expand(300, 7))
+    assert torch.equal(ent.view(300, 7), ent[:7].expand(300, 7))
+    want = ref.tokens(host(few), ids, np.zeros(7), np.zeros(7), 4, dtype)
+    ref.check(host(logp[:7]), want["logp"], "logp")
+    ref.check(host(ent[:7]), want["entropy"], "entropy")
+    ref.check(host(tl[-7:]), want["top_logp"], "top_logp")
+    assert np.array_equal(ti[:7].cpu().numpy(), want["top_ids"])
+
+
 @pytest.mark.parametrize("ids", ["u8", "i32", "i64"])
 def test_id_types_and_padding(ids):
     for A in (5, 300, 3001):
