@@ -864,6 +864,17 @@ __global__ void __launch_bounds__(256) draw_kernel(TokenArgs a) {
         alive = max(alive, __shfl_xor(alive, d, kLanes));
     }
     if (pick == kNoChoice) pick = alive;
+    float log_total = kLn2 * log2f(total);
+    if (__any(total < 1.5f)) {
+        // a row with one all but certain choice: log (1 + the others' weights), whose small numbers
+        // the 1 would leave no bits for
+        float others = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) others += v[i] < m ? exp2_of((v[i] - m) * kLog2e) : 0.0f;
+#pragma unroll
+        for (int d = kLanes / 2; d > 0; d >>= 1) others += __shfl_xor(others, d, kLanes);
+        if (total < 1.5f) log_total = log1pf(others);
+    }
     if (!live || lane != 0) return;
     float logp = kNone;
     if (!(total < __builtin_inff())) {                // a NaN, or a +inf
@@ -872,7 +883,7 @@ __global__ void __launch_bounds__(256) draw_kernel(TokenArgs a) {
     } else if (pick < 0) {
         pick = 0;
     } else {
-        logp = fmaf(-kLn2, log2f(total), to_f32(l[pick]) - m);
+        logp = to_f32(l[pick]) - m - log_total;
     }
     a.actions[row] = uint8_t(pick);
     if (a.logp) a.logp[row] = logp;

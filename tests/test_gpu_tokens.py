@@ -410,6 +410,25 @@ def test_draw_follows_the_distribution():
     assert (np.abs(count - p * N) <= 2).all() and count[1] == 0
 
 
+@pytest.mark.parametrize("A", [2, 5, 40, 200])
+def test_draw_of_a_certain_action(A):
+    """The log-probability of an action that is all but certain is small, and as exact as a large one.
+    Relative to it: the other weights by (1 + d) 2 U of themselves, d <= 12 the distance of their logits,
+    sixteen additions and the logarithm by 20 U."""
+    r = np.random.default_rng(A)
+    v = -r.uniform(9, 12, size=(300, A))
+    v[:, 0] = 0.0
+    v[7, 1] = 0.0                                # two of the largest
+    logits, u = torch.from_numpy(v).float().cuda(), np.zeros(300, dtype=np.float32)
+    actions = torch.empty(300, dtype=torch.uint8, device="cuda")
+    logp = torch.empty(300, device="cuda")
+    av.av_draw_actions(logits, torch.from_numpy(u).cuda(), actions, logp)
+    l = host(logits)
+    want = -np.log1p(np.exp(l[:, 1:]).sum(1))
+    assert not actions.any()
+    ref.check(host(logp), (want, ref.U * 46.0 * np.abs(want)), "logp")
+
+
 def test_draw_close_to_a_border():
     """Numbers at and next to the borders between choices, where 32 bits do not tell the side."""
     for A in (5, 64, 200):
