@@ -489,22 +489,23 @@ def _packed(t, name, dtype, shape, device):
     return t.data_ptr()
 
 
-def _workspace(size_of, name, config, args, workspace, device):
-    """The workspace's tensor (kept alive by the caller), address and size: the caller's, or a
-    new one from torch's allocator on the current stream."""
-    torch = _known[2]
+def _run(name, call, size_of, config, which, args, workspace, device):
+    """Makes a call that takes a workspace: the caller's, or, where it needs one (most do not, and one
+    that does is refused without before any device work), a new one from torch's allocator on the
+    current stream."""
     if workspace is None:
+        rc = call(config, *args, None, 0)
+        if rc == AV_OK:
+            return
         n = ctypes.c_size_t(0)
-        rc = size_of(config, *args, ctypes.byref(n))
-        if rc:
-            _check(name, rc)
-        if n.value == 0:
-            return None, None, 0
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
-    elif not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8 or \
+        if rc != AV_EINVAL or size_of(config, *which, ctypes.byref(n)) or n.value == 0:
+            _check(name, call(config, *args, None, 0) if rc == AV_EINVAL else rc)
+            return
+        workspace = _known[2].empty(n.value, dtype=_known[2].uint8, device=device)
+    elif not isinstance(workspace, _known[3]) or workspace.dtype != _known[2].uint8 or \
             not workspace.is_contiguous() or workspace.device != device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
-    return workspace, workspace.data_ptr(), workspace.numel()
+    _check(name, call(config, *args, workspace.data_ptr(), workspace.numel()))
 
 
 def _scan_common(x, gate, cut, form):
@@ -560,10 +561,8 @@ def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=Fal
     c = _SCAN.pack(*shape, kind, form, 1 if reverse else 0, per_value, sx[0], sx[1], sg[0], sg[1],
                    sy[0], sy[1], sc[0], sc[1], 0, 0, 0, 0, 0, 0, device.index, 0,
                    stream(device.index))
-    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", c, (0,), workspace, device)
-    rc = lib.av_scan(c, px, pg, pc, ph, py, pl, pw, n)
-    if rc:
-        _check("av_scan", rc)
+    _run("av_scan", lib.av_scan, lib.av_scan_workspace, c, (0,), (px, pg, pc, ph, py, pl), workspace,
+         device)
 
 
 def av_scan_backward(x, gate, y, dy, dx, dgate=None, h0=None, dlast=None, dh0=None, cut=None,
@@ -588,10 +587,8 @@ def av_scan_backward(x, gate, y, dy, dx, dgate=None, h0=None, dlast=None, dh0=No
     c = _SCAN.pack(*shape, kind, form, 1 if reverse else 0, per_value, sx[0], sx[1], sg[0], sg[1],
                    sy[0], sy[1], sc[0], sc[1], sdy[0], sdy[1], sdx[0], sdx[1], sdg[0], sdg[1],
                    device.index, 0, stream(device.index))
-    keep, pw, n = _workspace(lib.av_scan_workspace, "av_scan_workspace", c, (1,), workspace, device)
-    rc = lib.av_scan_backward(c, px, pg, pc, ph, py, pdy, pdl, pdx, pdg, pdh, pw, n)
-    if rc:
-        _check("av_scan_backward", rc)
+    _run("av_scan_backward", lib.av_scan_backward, lib.av_scan_workspace, c, (1,),
+         (px, pg, pc, ph, py, pdy, pdl, pdx, pdg, pdh), workspace, device)
 
 
 def _logits(logits):
@@ -650,11 +647,8 @@ def av_log_probs(logits, ids=None, logp=None, entropy=None, stats=None, top_logp
         pti = _packed(top_ids, "top_ids", torch.int32, (N, top), device)
     c = _TOKENS.pack(N, shape[1], kind, ids_type, stride, 0, top, device.index,
                      stream(device.index))
-    keep, pw, n = _workspace(lib.av_log_probs_workspace, "av_log_probs_workspace", c, (), workspace,
-                             device)
-    rc = lib.av_log_probs(c, pl, pi, plp, pe, ps, ptl, pti, pw, n)
-    if rc:
-        _check("av_log_probs", rc)
+    _run("av_log_probs", lib.av_log_probs, lib.av_log_probs_workspace, c, (),
+         (pl, pi, plp, pe, ps, ptl, pti), workspace, device)
 
 
 def av_log_probs_backward(logits, ids, stats, entropy, dlogp, dentropy, dlogits):
