@@ -335,6 +335,7 @@ hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool 
 
 struct TokenArgs {
     int64_t N, stride, dstride;       // rows, and the rows' strides in elements
+    int64_t all;                      // rows of the whole call, of which these are a run
     int A, top, ids_type, parts;
     const void *logits, *ids;
     float *logp, *entropy, *stats, *top_logp;

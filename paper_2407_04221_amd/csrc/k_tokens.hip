@@ -28,6 +28,13 @@ constexpr int kWaveRow = 4096;
 // Longest row of one wave in the gradient, in 16-byte words: longer ones give each thread of a workgroup
 // a word (50000 x 2040 in f32: 205 us as waves, so 139; x 1600 in bf16: 60 and 70).
 constexpr int kTeamBack = 256;
+// Words of all rows from which few lanes take a row, with several words each: fewer reductions and row
+// results an instruction, but fewer waves.  (300000 x 148 in f32: 84 us as waves, so 37; 8000 of them
+// 4.1 and 3.3; 8000 x 30 in f32 3.4 and 3.2, 8000 x 113 in f16 3.3 and 3.6.)  The gradient four times as
+// many, where the lanes' idle words are more than the last of a line (300000 x 66 in f16: 26.7 us, so
+// 18.8; x 148 in f32 114 and 69; but x 113 in f16, fifteen of sixteen lanes, 30.0 and 34.4 to 46; 30000 x
+// 148 in f32 10.2 and 8.9; 8000 x 300 in f16 5.3 and 5.0, x 256 in f32 4.4 and 5.3).
+constexpr int64_t kMany = int64_t(1) << 18;
 constexpr float kNone = -__builtin_inff();
 
 __device__ inline int64_t id_of(const TokenArgs &a, int64_t row) {
@@ -310,13 +317,14 @@ template <typename T> struct Words {
         for (int i = 0; i < kPer; ++i) v[i] = i >= from ? to_f32(q.v[i]) : kNone;
     }
     // Stores the gradients of a word.
-    __device__ void put(T *d, int word, const float (&v)[kPer]) const {
+    template <bool kPast> __device__ void put(T *d, int word, const float (&v)[kPer]) const {
         const int at = first(word), from = skip(word);
         Word<T, kPer> o;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) o.v[i] = from_f32<T>(v[i]);
         if (from == 0) {
-            store_past(d + at, o);
+            if (kPast) store_past(d + at, o);
+            else __builtin_memcpy(d + at, &o, sizeof o);
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
@@ -355,35 +363,51 @@ template <int kLanes> __device__ inline float team_sum(float v) {
     }));
 }
 
-// The alternatives of a row that kLanes lanes hold, one word each: the largest left of all lanes, again
-// and again; of equal ones the lowest lane and element has the lowest index.
-template <int kLanes, int kPer, typename Index>
-__device__ inline void largest_first(const TokenArgs &a, const Row &r, int64_t row, bool live, int lane,
-                                     const float (&v)[kPer], Index index) {
-    uint32_t key[kPer];
+// The alternatives of a row that kLanes lanes hold, kWords words each: the largest left of all lanes,
+// again and again, of equal ones the one of the lowest index.
+template <int kLanes, int kWords, int kPer, typename Index>
+__device__ inline void largest_first(const TokenArgs &a, const Row &r, int64_t row, bool live,
+                                     const float (&v)[kWords][kPer], Index index) {
+    const int lane = threadIdx.x % kLanes;
+    uint32_t key[kWords][kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) key[i] = uint32_t(key_of(v[i], 0) >> 32);
+    for (int w = 0; w < kWords; ++w)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[w][i] = uint32_t(key_of(v[w][i], 0) >> 32);
     const int shift = int(threadIdx.x & 63) / kLanes * kLanes;        // the team's first lane
     for (int j = 0; j < a.top; ++j) {
-        uint32_t best = key[0];
+        uint32_t best = 0;
 #pragma unroll
-        for (int i = 1; i < kPer; ++i) best = max(best, key[i]);
+        for (int w = 0; w < kWords; ++w)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) best = max(best, key[w][i]);
         uint32_t top;
         if constexpr (kLanes == 64) top = wave_max(best);
         else top = over_team<kLanes>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
-        const uint64_t team = __ballot(best == top) >> shift & (~uint64_t(0) >> (64 - kLanes));
-        if (lane != __ffsll(static_cast<unsigned long long>(team)) - 1) continue;
-        int which = kPer - 1;
+        int which = 0;                                  // the lane's first of them
 #pragma unroll
-        for (int i = kPer - 2; i >= 0; --i) which = key[i] == top ? i : which;
+        for (int w = kWords - 1; w >= 0; --w)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) key[i] = i == which ? 0 : key[i];
-        if (live) put_top(a, r, row, j, top ? uint64_t(top) << 32 | uint32_t(~index(which)) : 0);
+            for (int i = kPer - 1; i >= 0; --i) which = key[w][i] == top ? w * kPer + i : which;
+        const uint32_t at = best == top ? uint32_t(index(which / kPer, which % kPer)) : ~0u;
+        bool mine;
+        if constexpr (kWords == 1) {                    // the first lane's
+            const uint64_t team = __ballot(best == top) >> shift & (~uint64_t(0) >> (64 - kLanes));
+            mine = lane == __ffsll(static_cast<unsigned long long>(team)) - 1;
+        } else {
+            mine = at == over_team<kLanes>(at, [](uint32_t x, uint32_t y) { return min(x, y); });
+        }
+        if (!mine) continue;
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) key[w][i] = w * kPer + i == which ? 0 : key[w][i];
+        if (live) put_top(a, r, row, j, top ? uint64_t(top) << 32 | uint32_t(~at) : 0);
     }
 }
 
-// Rows of at most kLanes words, kLanes (4 to 32) lanes each and a word a lane.
-template <typename T, int kLanes>
+// Rows of at most kLanes kWords words, kLanes (4 to 32) lanes each and kWords words a lane.
+template <typename T, int kLanes, int kWords>
 __global__ void __launch_bounds__(256) team_rows_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
     const int lane = threadIdx.x % kLanes;
@@ -393,17 +417,23 @@ __global__ void __launch_bounds__(256) team_rows_kernel(TokenArgs a) {
     const Words<T> in(a, row);
     Given given{};
     if (lane == 0) given = given_of(a, row, in.l);
-    float v[kPer];
-    in.load(lane, v);
-    Stat st{team_max<kLanes>(largest(v)), 0.0f, 0.0f};
+    float v[kWords][kPer], m = kNone;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) add(st, v[i]);
+    for (int j = 0; j < kWords; ++j) in.load(j * kLanes + lane, v[j]);
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) m = fmaxf(m, largest(v[j]));
+    Stat st{team_max<kLanes>(m), 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < kWords; ++j)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) add(st, v[j][i]);
     st.s = team_sum<kLanes>(st.s);
     st.w = team_sum<kLanes>(st.w);
     const Row r = row_of(st);
     if (lane == 0 && live) put_row(a, r, row, given);
     if (a.top == 0) return;
-    largest_first<kLanes>(a, r, row, live, lane, v, [&](int i) { return in.first(lane) + i; });
+    largest_first<kLanes>(a, r, row, live, v,
+                          [&](int j, int i) { return in.first(j * kLanes + lane) + i; });
 }
 
 // The k-th largest of the wave's 64 numbers (0 if fewer are set): bit by bit from the top, the
@@ -461,8 +491,8 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
     const Row r = row_of(st);
     if (lane == 0) put_row(a, r, row, given);
     if (a.top == 0) return;
-    if (kWords == 1 && a.top <= kFew) {
-        largest_first<64>(a, r, row, true, lane, v[0], [&](int i) { return in.first(lane) + i; });
+    if constexpr (kWords == 1) if (a.top <= kFew) {
+        largest_first<64>(a, r, row, true, v, [&](int, int i) { return in.first(lane) + i; });
         return;
     }
     if (kWords <= kFewWords && a.top == 1) {
@@ -756,12 +786,15 @@ __global__ void __launch_bounds__(256) long_back_kernel(TokenArgs a) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) v[i] = to_f32(q.v[i]);
         slopes(b, in.first(word), v);
-        in.put(d, word, v);
+        in.template put<true>(d, word, v);
     }
 }
 
-// The same for rows of at most kTeamBack words, kLanes lanes each.
-template <typename T, int kLanes>
+// The same for rows of at most kTeamBack words, kLanes lanes each and kWords words a lane on their way.  A
+// lane with one word has the whole row's stores in one instruction, which may go past the caches;
+// several leave lines in pieces, which the caches put together (300000 x 148 in f32: 69 us, past
+// them 83).
+template <typename T, int kLanes, int kWords>
 __global__ void __launch_bounds__(256) team_back_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
     const int64_t row = int64_t(blockIdx.x) * (256 / kLanes) + threadIdx.x / kLanes;
@@ -769,13 +802,20 @@ __global__ void __launch_bounds__(256) team_back_kernel(TokenArgs a) {
     const Words<T> in(a, row);
     T *d = static_cast<T *>(a.dlogits) + row * a.dstride;
     const Back b = back_of(a, row);
-    for (int word = threadIdx.x % kLanes; word < in.count; word += kLanes) {
-        const Word<T, kPer> q = in.get(word);
-        float v[kPer];
+    for (int word = threadIdx.x % kLanes; word < in.count; word += kLanes * kWords) {
+        Word<T, kPer> q[kWords];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = to_f32(q.v[i]);
-        slopes(b, in.first(word), v);
-        in.put(d, word, v);
+        for (int j = 0; j < kWords; ++j) q[j] = in.get(min(word + j * kLanes, in.count - 1));
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            const int at = word + j * kLanes;
+            if (at >= in.count) continue;
+            float v[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) v[i] = to_f32(q[j].v[i]);
+            slopes(b, in.first(at), v);
+            in.template put<kWords == 1>(d, at, v);
+        }
     }
 }
 
@@ -926,10 +966,18 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
     const int words = words_of<T>(a);
     if (a.A <= kWaveRow) {
         auto rows = [&](int lanes) { return dim3(blocks_of(a.N, 256 / lanes)); };
-        if (words <= 4) hipLaunchKernelGGL((team_rows_kernel<T, 4>), rows(4), b, 0, s, a);
-        else if (words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 8>), rows(8), b, 0, s, a);
-        else if (words <= 16) hipLaunchKernelGGL((team_rows_kernel<T, 16>), rows(16), b, 0, s, a);
-        else if (words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 32>), rows(32), b, 0, s, a);
+        const bool many = a.all * words >= kMany, few = a.top <= kFew;
+        if (words <= 4) hipLaunchKernelGGL((team_rows_kernel<T, 4, 1>), rows(4), b, 0, s, a);
+        else if (many && words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 4, 2>), rows(4), b, 0, s, a);
+        else if (many && words <= 12) hipLaunchKernelGGL((team_rows_kernel<T, 4, 3>), rows(4), b, 0, s, a);
+        else if (many && words <= 16) hipLaunchKernelGGL((team_rows_kernel<T, 4, 4>), rows(4), b, 0, s, a);
+        else if (many && words <= 24) hipLaunchKernelGGL((team_rows_kernel<T, 8, 3>), rows(8), b, 0, s, a);
+        else if (many && words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 8, 4>), rows(8), b, 0, s, a);
+        else if (many && few && words <= 48) hipLaunchKernelGGL((team_rows_kernel<T, 16, 3>), rows(16), b, 0, s, a);
+        else if (many && few && words <= 64) hipLaunchKernelGGL((team_rows_kernel<T, 16, 4>), rows(16), b, 0, s, a);
+        else if (words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 8, 1>), rows(8), b, 0, s, a);
+        else if (words <= 16) hipLaunchKernelGGL((team_rows_kernel<T, 16, 1>), rows(16), b, 0, s, a);
+        else if (words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 32, 1>), rows(32), b, 0, s, a);
         else if (words <= 64) hipLaunchKernelGGL((wave_rows_kernel<T, 1>), rows(64), b, 0, s, a);
         else if (words <= 128) hipLaunchKernelGGL((wave_rows_kernel<T, 2>), rows(64), b, 0, s, a);
         else if (words <= 256) hipLaunchKernelGGL((wave_rows_kernel<T, 4>), rows(64), b, 0, s, a);
@@ -967,11 +1015,18 @@ template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
     const int words = words_of<T>(a);
     if (words <= kTeamBack) {
         auto rows = [&](int lanes) { return dim3(blocks_of(a.N, 256 / lanes)); };
-        if (words <= 4) hipLaunchKernelGGL((team_back_kernel<T, 4>), rows(4), b, 0, s, a);
-        else if (words <= 8) hipLaunchKernelGGL((team_back_kernel<T, 8>), rows(8), b, 0, s, a);
-        else if (words <= 16) hipLaunchKernelGGL((team_back_kernel<T, 16>), rows(16), b, 0, s, a);
-        else if (words <= 32) hipLaunchKernelGGL((team_back_kernel<T, 32>), rows(32), b, 0, s, a);
-        else hipLaunchKernelGGL((team_back_kernel<T, 64>), rows(64), b, 0, s, a);
+        const bool many = a.all * words >= 4 * kMany;
+        if (words <= 4) hipLaunchKernelGGL((team_back_kernel<T, 4, 1>), rows(4), b, 0, s, a);
+        else if (words <= 8) hipLaunchKernelGGL((team_back_kernel<T, 8, 1>), rows(8), b, 0, s, a);
+        else if (many && words <= 12) hipLaunchKernelGGL((team_back_kernel<T, 4, 3>), rows(4), b, 0, s, a);
+        else if (words <= 16) hipLaunchKernelGGL((team_back_kernel<T, 16, 1>), rows(16), b, 0, s, a);
+        else if (many && words <= 24) hipLaunchKernelGGL((team_back_kernel<T, 8, 3>), rows(8), b, 0, s, a);
+        else if (many && words <= 32) hipLaunchKernelGGL((team_back_kernel<T, 16, 2>), rows(16), b, 0, s, a);
+        else if (many && words <= 48) hipLaunchKernelGGL((team_back_kernel<T, 16, 3>), rows(16), b, 0, s, a);
+        else if (many && words <= 64) hipLaunchKernelGGL((team_back_kernel<T, 16, 4>), rows(16), b, 0, s, a);
+        else if (many && words <= 96) hipLaunchKernelGGL((team_back_kernel<T, 32, 3>), rows(32), b, 0, s, a);
+        else if (words <= 32) hipLaunchKernelGGL((team_back_kernel<T, 32, 1>), rows(32), b, 0, s, a);
+        else hipLaunchKernelGGL((team_back_kernel<T, 64, 1>), rows(64), b, 0, s, a);
         return hipGetLastError();
     }
     // enough workgroups for the device where the rows are few
@@ -1015,6 +1070,7 @@ template <typename F> static hipError_t in_runs(const TokenArgs &all, int dtype,
     for (int64_t row = 0; row < all.N; row += kRun) {
         TokenArgs a = all;
         a.N = std::min(kRun, all.N - row);
+        a.all = all.N;
         a.logits = static_cast<const char *>(all.logits) + row * all.stride * size;
         if (all.ids) a.ids = static_cast<const char *>(all.ids) + row * id;
         if (all.logp) a.logp += row;
