@@ -30,7 +30,9 @@ constexpr int kWaveRow = 4096;
 constexpr int kTeamBack = 256;
 // Words of all rows from which few lanes take a row, with several words each: fewer reductions and row
 // results an instruction, but fewer waves.  (300000 x 148 in f32: 84 us as waves, so 37; 8000 of them
-// 4.1 and 3.3; 8000 x 30 in f32 3.4 and 3.2, 8000 x 113 in f16 3.3 and 3.6.)  The gradient four times as
+// 4.1 and 3.3; 8000 x 30 in f32 3.4 and 3.2, 8000 x 113 in f16 3.3 and 3.6.)  With alternatives, which cost
+// each lane its words, up to 64 words (200000 x 1000 in f16, 32 lanes or a wave: none 83 and 97, four
+// of them 193 and 156).  The gradient four times as
 // many, where the lanes' idle words are more than the last of a line (300000 x 66 in f16: 26.7 us, so
 // 18.8; x 148 in f32 114 and 69; but x 113 in f16, fifteen of sixteen lanes, 30.0 and 34.4 to 46; 30000 x
 // 148 in f32 10.2 and 8.9; 8000 x 300 in f16 5.3 and 5.0, x 256 in f32 4.4 and 5.3).
@@ -975,11 +977,14 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
         else if (many && words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 8, 4>), rows(8), b, 0, s, a);
         else if (many && few && words <= 48) hipLaunchKernelGGL((team_rows_kernel<T, 16, 3>), rows(16), b, 0, s, a);
         else if (many && few && words <= 64) hipLaunchKernelGGL((team_rows_kernel<T, 16, 4>), rows(16), b, 0, s, a);
+        else if (many && a.top == 0 && words <= 96) hipLaunchKernelGGL((team_rows_kernel<T, 32, 3>), rows(32), b, 0, s, a);
+        else if (many && a.top == 0 && words <= 128) hipLaunchKernelGGL((team_rows_kernel<T, 32, 4>), rows(32), b, 0, s, a);
         else if (words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 8, 1>), rows(8), b, 0, s, a);
         else if (words <= 16) hipLaunchKernelGGL((team_rows_kernel<T, 16, 1>), rows(16), b, 0, s, a);
         else if (words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 32, 1>), rows(32), b, 0, s, a);
         else if (words <= 64) hipLaunchKernelGGL((wave_rows_kernel<T, 1>), rows(64), b, 0, s, a);
         else if (words <= 128) hipLaunchKernelGGL((wave_rows_kernel<T, 2>), rows(64), b, 0, s, a);
+        else if (words <= 192) hipLaunchKernelGGL((wave_rows_kernel<T, 3>), rows(64), b, 0, s, a);
         else if (words <= 256) hipLaunchKernelGGL((wave_rows_kernel<T, 4>), rows(64), b, 0, s, a);
         else if (words <= 384) hipLaunchKernelGGL((wave_rows_kernel<T, 6>), rows(64), b, 0, s, a);
         else if (words <= 512) hipLaunchKernelGGL((wave_rows_kernel<T, 8>), rows(64), b, 0, s, a);

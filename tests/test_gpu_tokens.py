@@ -129,6 +129,9 @@ def test_many_rows_of_medium_length(A, dtype):
         for t in (logp, ent, tl, ti):
             same = t.view(torch.int32).view(times, 61, -1)
             assert torch.equal(same, same[:1].expand_as(same))
+    av.av_log_probs(logits, many(ids), logp, ent, stats)
+    ref.check(host(logp[:61]), want["logp"], "logp")
+    ref.check(host(ent[:61]), want["entropy"], "entropy")
     d = torch.empty_like(logits)
     av.av_log_probs_backward(logits, many(ids), stats, ent, many(g), many(gh), d)
     ref.check(host(d[:61]), want["dlogits"], "dlogits", dtype)
