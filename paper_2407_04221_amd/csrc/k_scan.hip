@@ -164,11 +164,14 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEa
     float ca[V], cr[V];                       // a gate per value: a and 1 - a
 
     __device__ Reader(const ScanArgs &p, const Column &c, uint32_t b0)
-        : x(p.x, p.x_step, p.x_row, sizeof(T), b0, c), g(p.gate, p.gate_step, p.gate_row, sizeof(T), b0, c, !kCol),
-          e(kBack ? p.dy : p.x, kBack ? p.dy_step : p.x_step, kBack ? p.dy_row : p.x_row, sizeof(T), b0, c),
+        : x(p.x, p.x_step, p.x_row, sizeof(T), b0, c),
+          g(p.gate, p.gate_step, p.gate_row, sizeof(T), b0, c, !kCol),
+          e(kBack ? p.dy : p.x, kBack ? p.dy_step : p.x_step, kBack ? p.dy_row : p.x_row, sizeof(T),
+            b0, c),
           y(p.y, p.y_step, p.y_row, sizeof(T), b0, c),
-          cut(p.cut, p.cut_step, p.cut_row, 1, b0, Column{c.n, 0, c.live, c.b, p.each ? c.d : 0, false}), steps(int(p.T)),
-          cuts(p.cut != nullptr) {
+          cut(p.cut, p.cut_step, p.cut_row, 1, b0,
+              Column{c.n, 0, c.live, c.b, p.each ? c.d : 0, false}),
+          steps(int(p.T)), cuts(p.cut != nullptr) {
         if (kCol) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {

@@ -970,15 +970,24 @@ template <typename T> hipError_t forward(const TokenArgs &a, hipStream_t s) {
         auto rows = [&](int lanes) { return dim3(blocks_of(a.N, 256 / lanes)); };
         const bool many = a.all * words >= kMany, few = a.top <= kFew;
         if (words <= 4) hipLaunchKernelGGL((team_rows_kernel<T, 4, 1>), rows(4), b, 0, s, a);
-        else if (many && words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 4, 2>), rows(4), b, 0, s, a);
-        else if (many && words <= 12) hipLaunchKernelGGL((team_rows_kernel<T, 4, 3>), rows(4), b, 0, s, a);
-        else if (many && words <= 16) hipLaunchKernelGGL((team_rows_kernel<T, 4, 4>), rows(4), b, 0, s, a);
-        else if (many && words <= 24) hipLaunchKernelGGL((team_rows_kernel<T, 8, 3>), rows(8), b, 0, s, a);
-        else if (many && words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 8, 4>), rows(8), b, 0, s, a);
-        else if (many && few && words <= 48) hipLaunchKernelGGL((team_rows_kernel<T, 16, 3>), rows(16), b, 0, s, a);
-        else if (many && few && words <= 64) hipLaunchKernelGGL((team_rows_kernel<T, 16, 4>), rows(16), b, 0, s, a);
-        else if (many && a.top == 0 && words <= 96) hipLaunchKernelGGL((team_rows_kernel<T, 32, 3>), rows(32), b, 0, s, a);
-        else if (many && a.top == 0 && words <= 128) hipLaunchKernelGGL((team_rows_kernel<T, 32, 4>), rows(32), b, 0, s, a);
+        else if (many && words <= 8)
+            hipLaunchKernelGGL((team_rows_kernel<T, 4, 2>), rows(4), b, 0, s, a);
+        else if (many && words <= 12)
+            hipLaunchKernelGGL((team_rows_kernel<T, 4, 3>), rows(4), b, 0, s, a);
+        else if (many && words <= 16)
+            hipLaunchKernelGGL((team_rows_kernel<T, 4, 4>), rows(4), b, 0, s, a);
+        else if (many && words <= 24)
+            hipLaunchKernelGGL((team_rows_kernel<T, 8, 3>), rows(8), b, 0, s, a);
+        else if (many && words <= 32)
+            hipLaunchKernelGGL((team_rows_kernel<T, 8, 4>), rows(8), b, 0, s, a);
+        else if (many && few && words <= 48)
+            hipLaunchKernelGGL((team_rows_kernel<T, 16, 3>), rows(16), b, 0, s, a);
+        else if (many && few && words <= 64)
+            hipLaunchKernelGGL((team_rows_kernel<T, 16, 4>), rows(16), b, 0, s, a);
+        else if (many && a.top == 0 && words <= 96)
+            hipLaunchKernelGGL((team_rows_kernel<T, 32, 3>), rows(32), b, 0, s, a);
+        else if (many && a.top == 0 && words <= 128)
+            hipLaunchKernelGGL((team_rows_kernel<T, 32, 4>), rows(32), b, 0, s, a);
         else if (words <= 8) hipLaunchKernelGGL((team_rows_kernel<T, 8, 1>), rows(8), b, 0, s, a);
         else if (words <= 16) hipLaunchKernelGGL((team_rows_kernel<T, 16, 1>), rows(16), b, 0, s, a);
         else if (words <= 32) hipLaunchKernelGGL((team_rows_kernel<T, 32, 1>), rows(32), b, 0, s, a);
@@ -1023,13 +1032,19 @@ template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
         const bool many = a.all * words >= 4 * kMany;
         if (words <= 4) hipLaunchKernelGGL((team_back_kernel<T, 4, 1>), rows(4), b, 0, s, a);
         else if (words <= 8) hipLaunchKernelGGL((team_back_kernel<T, 8, 1>), rows(8), b, 0, s, a);
-        else if (many && words <= 12) hipLaunchKernelGGL((team_back_kernel<T, 4, 3>), rows(4), b, 0, s, a);
+        else if (many && words <= 12)
+            hipLaunchKernelGGL((team_back_kernel<T, 4, 3>), rows(4), b, 0, s, a);
         else if (words <= 16) hipLaunchKernelGGL((team_back_kernel<T, 16, 1>), rows(16), b, 0, s, a);
-        else if (many && words <= 24) hipLaunchKernelGGL((team_back_kernel<T, 8, 3>), rows(8), b, 0, s, a);
-        else if (many && words <= 32) hipLaunchKernelGGL((team_back_kernel<T, 16, 2>), rows(16), b, 0, s, a);
-        else if (many && words <= 48) hipLaunchKernelGGL((team_back_kernel<T, 16, 3>), rows(16), b, 0, s, a);
-        else if (many && words <= 64) hipLaunchKernelGGL((team_back_kernel<T, 16, 4>), rows(16), b, 0, s, a);
-        else if (many && words <= 96) hipLaunchKernelGGL((team_back_kernel<T, 32, 3>), rows(32), b, 0, s, a);
+        else if (many && words <= 24)
+            hipLaunchKernelGGL((team_back_kernel<T, 8, 3>), rows(8), b, 0, s, a);
+        else if (many && words <= 32)
+            hipLaunchKernelGGL((team_back_kernel<T, 16, 2>), rows(16), b, 0, s, a);
+        else if (many && words <= 48)
+            hipLaunchKernelGGL((team_back_kernel<T, 16, 3>), rows(16), b, 0, s, a);
+        else if (many && words <= 64)
+            hipLaunchKernelGGL((team_back_kernel<T, 16, 4>), rows(16), b, 0, s, a);
+        else if (many && words <= 96)
+            hipLaunchKernelGGL((team_back_kernel<T, 32, 3>), rows(32), b, 0, s, a);
         else if (words <= 32) hipLaunchKernelGGL((team_back_kernel<T, 32, 1>), rows(32), b, 0, s, a);
         else hipLaunchKernelGGL((team_back_kernel<T, 64, 1>), rows(64), b, 0, s, a);
         return hipGetLastError();
@@ -1044,8 +1059,10 @@ template <typename T> hipError_t backward(const TokenArgs &a, hipStream_t s) {
 template <typename T> hipError_t draw(const TokenArgs &a, hipStream_t s) {
     const dim3 b(256);
     if (a.A <= 8) hipLaunchKernelGGL((draw_kernel<T, 2, 4>), dim3(blocks_of(a.N, 128)), b, 0, s, a);
-    else if (a.A <= 64) hipLaunchKernelGGL((draw_kernel<T, 8, 8>), dim3(blocks_of(a.N, 32)), b, 0, s, a);
-    else if (a.A <= 128) hipLaunchKernelGGL((draw_kernel<T, 16, 8>), dim3(blocks_of(a.N, 16)), b, 0, s, a);
+    else if (a.A <= 64)
+        hipLaunchKernelGGL((draw_kernel<T, 8, 8>), dim3(blocks_of(a.N, 32)), b, 0, s, a);
+    else if (a.A <= 128)
+        hipLaunchKernelGGL((draw_kernel<T, 16, 8>), dim3(blocks_of(a.N, 16)), b, 0, s, a);
     else hipLaunchKernelGGL((draw_kernel<T, 32, 8>), dim3(blocks_of(a.N, 8)), b, 0, s, a);
     return hipGetLastError();
 }
