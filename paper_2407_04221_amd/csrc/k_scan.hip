@@ -344,7 +344,7 @@ template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
 __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     constexpr int K = steps_of(V), kMost = waves_of(V);
     // Loading a tile ahead pays where few workgroups share a compute unit; with many it only
-    // costs registers, in the gradient too many (128 x 1024 x 256 in bf16: 85 us, without 81).
+    // costs registers, in the gradient too many (128 x 1024 x 256 in bf16: 92 us, without 80).
     constexpr bool kAhead = V == 1 || !kBack;
     __shared__ float2 spans[2][kMost * 64 * V];
     __shared__ float carry[2][64 * V];        // the state after a tile, for the next one

@@ -773,7 +773,7 @@ template <typename T> __global__ void __launch_bounds__(256) join_rows_kernel(To
 
 // Gradient of rows of any length; blockIdx.y, and the threads, share a row's words.  The gradient
 // goes past the caches: it is not read again here, and the logits, which the forward pass has just
-// read, stay (4096 x 32768 in bf16, both passes: 169 us, so 142).
+// read, stay (4096 x 32768 in bf16, both passes: 169 us, so 139).
 template <typename T>
 __global__ void __launch_bounds__(256) long_back_kernel(TokenArgs a) {
     constexpr int kPer = Words<T>::kPer;
