@@ -526,7 +526,9 @@ av_status av_log_probs_workspace(const av_tokens_config *cfg, size_t *bytes);
  *   top_logp, top_ids   device float / int32 [N][top], log-probability falling, of equal ones
  *             the lowest index first; with top = 0 not used, else neither may be NULL.
  * A logit of -infinity is a masked choice: probability 0, no part in entropy or alternatives
- * (places left over get id -1 and -infinity).  A row without any other has logp -infinity,
+ * (places left over get id -1 and -infinity).  The small logp and entropy of an all but certain
+ * choice, and the 1 - p of its gradient, are as exact relative to themselves as large ones are.
+ * A row without any other has logp -infinity,
  * entropy 0.  A row holding a NaN or +infinity has NaN results and ids -1.
  * workspace: av_log_probs_workspace bytes or more, 16-byte aligned, not shared by calls that may
  * overlap; NULL where that is 0 (it is for all but a few long rows). */

@@ -4,7 +4,11 @@
 // With m the row's largest logit and L = log2 e,
 //   t_i = (l_i - m) L,  S = sum 2^t_i,  w = sum t_i 2^t_i,
 //   log p_i = (l_i - m) - ln 2 log2 S,  H = ln 2 (log2 S - w / S);
-// the gradient is given (m, log2 S).  The difference is taken before the multiplication: l L - m L
+// the gradient is given (m, log2 S).  An S below 1.5 is 1, the largest itself, and little else: the
+// others are then summed on their own, R = S - 1, so that log2 S = log2 e log1p R keeps the bits that
+// 1 + R drops (logits 0 and four of -16: log p = -4.50e-7, from the sum -4.77e-7), and with it log p
+// and H, which is a sum of two terms that are not negative.  (1638400 rows of 5 in f32, many of them like
+// this, both ways: 29.6 us, without 29.2.)  The difference is taken before the multiplication: l L - m L
 // as one fused operation is shorter, but m L passes the largest number where all logits are the
 // type's lowest.  A masked choice has t = -inf and adds nothing; t is bounded below in the product
 // t 2^t so that its 0 is not -inf x 0.  A NaN or +inf among the logits makes S a NaN.
@@ -62,11 +66,12 @@ __device__ inline void raise(Stat &a, float m) {
     a.m = m;
 }
 
-__device__ inline void add(Stat &a, float l) {
+__device__ inline float add(Stat &a, float l) {
     const float t = (l - origin(a.m)) * kLog2e;
     const float e = exp2_of(t);
     a.s += e;
     a.w = fmaf(fmaxf(t, -1.0e4f), e, a.w);
+    return e;
 }
 
 // Reductions over a wave by DPP: within rows of 16 lanes, then lane 15 of a row into the next and
@@ -110,14 +115,32 @@ __device__ inline Stat join_lanes(Stat a) {
     return a;
 }
 
-// The row's results from its (m, S, w).
+// Whether a row's results, or a part's sums, are worked out from the weights of all but the largest.
+__device__ inline bool certain(float s) { return s < 1.5f; }
+__device__ inline float weight_below(float l, float m) {
+    return l < m ? exp2_of((l - m) * kLog2e) : 0.0f;
+}
+
+// log (1 + x) for 0 <= x <= 1/2, twice the area hyperbolic tangent of z = x / (2 + x) <= 1/5: z (1 + z^2 / 3 +
+// .. + z^10 / 11), of which the next term is 3e-10.  Within 4 roundings of itself.
+__device__ inline float log1p_half(float x) {
+    const float z = x * __builtin_amdgcn_rcpf(2.0f + x), q = z * z;
+    float s = fmaf(1.0f / 11.0f, q, 1.0f / 9.0f);
+    s = fmaf(s, q, 1.0f / 7.0f);
+    s = fmaf(s, q, 0.2f);
+    s = fmaf(s, q, 1.0f / 3.0f);
+    return 2.0f * fmaf(z * q, s, z);
+}
+
+// The row's results from its (m, S, w), and, where S is certain(), S - 1.
 struct Row { float m, lse, entropy; bool bad; };
 
-__device__ inline Row row_of(const Stat &a) {
+__device__ inline Row row_of(const Stat &a, float others) {
     Row r;
     r.m = origin(a.m);
     r.bad = !(a.s < __builtin_inff());
-    r.lse = a.m == kNone ? 0.0f : log2f(a.s);
+    r.lse = certain(a.s) ? kLog2e * log1p_half(others) : log2f(a.s);
+    if (a.m == kNone) r.lse = 0.0f;
     r.entropy = a.m == kNone ? 0.0f : fmaxf(0.0f, kLn2 * (r.lse - a.w / a.s));
     if (r.bad) r.m = r.lse = r.entropy = __builtin_nanf("");
     return r;
@@ -207,11 +230,15 @@ __global__ void __launch_bounds__(256) small_rows_kernel(TokenArgs a) {
     float v[kA];
     load_small(l, a.A, v);
     Stat st{kNone, 0.0f, 0.0f};
+    float others = 0.0f;
 #pragma unroll
     for (int i = 0; i < kA; ++i) st.m = fmaxf(st.m, v[i]);
 #pragma unroll
-    for (int i = 0; i < kA; ++i) add(st, v[i]);
-    const Row r = row_of(st);
+    for (int i = 0; i < kA; ++i) {
+        const float e = add(st, v[i]);
+        others += v[i] < st.m ? e : 0.0f;
+    }
+    const Row r = row_of(st, others);
     put_row(a, r, row, given);
     if (a.top) {
         uint64_t last = ~uint64_t(0);
@@ -228,8 +255,9 @@ __global__ void __launch_bounds__(256) small_rows_kernel(TokenArgs a) {
     }
 }
 
-// What the gradient of one row needs: log2 p_i = (l - m) L - lse, d = p (c0 + c1 log2 p).
-struct Back { float m, lse, g, c0, c1; int id; };
+// What the gradient of one row needs: log2 p_i = (l - m) L - lse, d = p (c0 + c1 log2 p), and of the
+// given token p (ch + c1 log2 p) + g (1 - p).
+struct Back { float m, lse, g, c0, c1, ch; int id; };
 
 __device__ inline Back back_of(const TokenArgs &a, int64_t row) {
     Back b;
@@ -240,7 +268,8 @@ __device__ inline Back back_of(const TokenArgs &a, int64_t row) {
     b.g = b.id >= 0 ? a.dlogp[row] : 0.0f;
     const float gh = a.dentropy ? a.dentropy[row] : 0.0f;
     b.c1 = -gh * kLn2;
-    b.c0 = -b.g - (a.dentropy ? gh * a.in_entropy[row] : 0.0f);
+    b.ch = a.dentropy ? -gh * a.in_entropy[row] : 0.0f;
+    b.c0 = b.ch - b.g;
     return b;
 }
 
@@ -248,19 +277,33 @@ __device__ inline float slope(const Back &b, float l) {
     const float t = fmaf(l - b.m, kLog2e, -b.lse);
     return exp2_of(t) * fmaf(b.c1, fmaxf(t, -1.0e4f), b.c0);
 }
+// The given token's.  Of 1 - p little is left where p is all but 1: above e^-1/2 it is the series of
+// 1 - e^x, x = log p, up to x^9 / 9! (the next term is 5e-10 of it), within 3 roundings of itself.
+__device__ inline float own_slope(const Back &b, float l) {
+    const float t = fmaf(l - b.m, kLog2e, -b.lse), p = exp2_of(t), x = kLn2 * t;
+    float s = fmaf(1.0f / 362880.0f, x, 1.0f / 40320.0f);
+    s = fmaf(s, x, 1.0f / 5040.0f);
+    s = fmaf(s, x, 1.0f / 720.0f);
+    s = fmaf(s, x, 1.0f / 120.0f);
+    s = fmaf(s, x, 1.0f / 24.0f);
+    s = fmaf(s, x, 1.0f / 6.0f);
+    s = fmaf(s, x, 0.5f);
+    const float rest = x > -0.5f ? -fmaf(x * x, s, x) : 1.0f - p;
+    return fmaf(p, fmaf(b.c1, fmaxf(t, -1.0e4f), b.ch), b.g * rest);
+}
 
 // The gradients of n neighbouring choices from index `at` on.
 template <int n> __device__ inline void slopes(const Back &b, int at, float (&v)[n]) {
     const int own = b.id - at;                 // the given token among them, unless it is masked
-    float extra[n];
-    const bool here = b.id >= 0 && own >= 0 && own < n;
+    float mine = kNone;
 #pragma unroll
-    for (int i = 0; i < n; ++i) extra[i] = here && i == own && v[i] != kNone ? b.g : 0.0f;
+    for (int i = 0; i < n; ++i) mine = i == own ? v[i] : mine;
 #pragma unroll
     for (int i = 0; i < n; ++i) v[i] = slope(b, v[i]);
-    if (here) {
+    if (unsigned(own) < unsigned(n) && mine != kNone) {
+        mine = own_slope(b, mine);
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] += extra[i];
+        for (int i = 0; i < n; ++i) v[i] = i == own ? mine : v[i];
     }
 }
 
@@ -431,7 +474,15 @@ __global__ void __launch_bounds__(256) team_rows_kernel(TokenArgs a) {
         for (int i = 0; i < kPer; ++i) add(st, v[j][i]);
     st.s = team_sum<kLanes>(st.s);
     st.w = team_sum<kLanes>(st.w);
-    const Row r = row_of(st);
+    float others = 0.0f;
+    if (__any(certain(st.s))) {
+#pragma unroll
+        for (int j = 0; j < kWords; ++j)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) others += weight_below(v[j][i], st.m);
+        others = team_sum<kLanes>(others);
+    }
+    const Row r = row_of(st, others);
     if (lane == 0 && live) put_row(a, r, row, given);
     if (a.top == 0) return;
     largest_first<kLanes>(a, r, row, live, v,
@@ -490,7 +541,15 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
         for (int i = 0; i < kPer; ++i) add(st, v[j][i]);
     st.s = wave_sum(st.s);
     st.w = wave_sum(st.w);
-    const Row r = row_of(st);
+    float others = 0.0f;
+    if (certain(st.s)) {                                // the same in all lanes
+#pragma unroll
+        for (int j = 0; j < kWords; ++j)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) others += weight_below(v[j][i], st.m);
+        others = wave_sum(others);
+    }
+    const Row r = row_of(st, others);
     if (lane == 0) put_row(a, r, row, given);
     if (a.top == 0) return;
     if constexpr (kWords == 1) if (a.top <= kFew) {
@@ -656,7 +715,26 @@ __device__ void alternatives(const TokenArgs &a, const Parts<T> &in, float m, Pu
     }
 }
 
-// One workgroup per row of any length, or, kSplit, per part of it (blockIdx.y), whose sums and
+// The weights of a row's, or a part's, words below its largest, which all threads name.
+template <typename T, int kThreads>
+__device__ float others_of(const Parts<T> &in, float m) {
+    constexpr int kPer = Parts<T>::kPer, kWaves = kThreads / 64;
+    __shared__ float sums[kWaves];
+    const int lane = threadIdx.x & 63;
+    float e = 0.0f;
+    for (int word = in.from + threadIdx.x; word < in.to; word += kThreads) {
+        float v[kPer];
+        in.load(word, v);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) e += weight_below(v[i], m);
+    }
+    e = wave_sum(e);
+    if (lane == 0) sums[threadIdx.x >> 6] = e;
+    __syncthreads();
+    return wave_sum(lane < kWaves ? sums[lane] : 0.0f);
+}
+
+// One workgroup per row of any length, or, kSplit, per part of it (blockIdx.y), whose m, S - 1 and w and
 // alternatives go to the workspace.  A thread has kWords 16-byte words on their way at once; the
 // largest of their elements is found first, so that the sums are rescaled at most once for all.  Four
 // words, or eight for many long rows (2500 x 60001 in f32: 122 us, with four 129; but 777 x 50021 in
@@ -712,17 +790,19 @@ __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
     __syncthreads();
     Stat all{kNone, 0.0f, 0.0f};
     if (lane < kWaves) all = stats[lane];
-    all = join_lanes(all);
+    all = join_lanes(all);                              // the same in all waves
+    float others = all.s - 1.0f;
+    if (certain(all.s)) others = others_of<T, kThreads>(in, all.m);
     if (kSplit) {
         const int64_t at = row * a.parts + blockIdx.y;
-        if (tid == 0) static_cast<Stat *>(a.part_stats)[at] = all;
+        if (tid == 0) static_cast<Stat *>(a.part_stats)[at] = Stat{all.m, others, all.w};
         if (a.top) {
             uint64_t *keys = a.part_keys + at * a.top;
             alternatives<T, kThreads>(a, in, mine, [&](int place, uint64_t k) { keys[place] = k; });
         }
         return;
     }
-    const Row r = row_of(all);
+    const Row r = row_of(all, others);
     if (tid == 0) put_row(a, r, row, given);
     if (a.top)
         alternatives<T, kThreads>(a, in, mine, [&](int place, uint64_t k) {
@@ -751,7 +831,16 @@ template <typename T> __global__ void __launch_bounds__(256) join_rows_kernel(To
         given = given_of(a, row, static_cast<const T *>(a.logits) + row * a.stride);
         listed = 0;
     }
-    const Row r = row_of(join_lanes(all));
+    // what a part without a choice has for S - 1 is 0, or a NaN
+    const float rest = all.s;
+    all.s = all.m == kNone ? rest : 1.0f + rest;
+    Stat sum = all;
+    raise(sum, wave_max(all.m));
+    // of the one part with the row's largest, if the row is certain(), S - 1; of the others all
+    const float others = wave_sum(all.m == sum.m ? rest : sum.s);
+    sum.s = wave_sum(sum.s);
+    sum.w = wave_sum(sum.w);
+    const Row r = row_of(sum, others);
     if (tid == 0) put_row(a, r, row, given);
     if (a.top == 0) return;
     bound = max(wave_max(bound), uint64_t(1));
@@ -912,7 +1001,7 @@ __global__ void __launch_bounds__(256) draw_kernel(TokenArgs a) {
         // the 1 would leave no bits for
         float others = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) others += v[i] < m ? exp2_of((v[i] - m) * kLog2e) : 0.0f;
+        for (int i = 0; i < kEach; ++i) others += weight_below(v[i], m);
 #pragma unroll
         for (int d = kLanes / 2; d > 0; d >>= 1) others += __shfl_xor(others, d, kLanes);
         if (total < 1.5f) log_total = log1pf(others);
