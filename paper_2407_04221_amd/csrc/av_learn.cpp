@@ -133,10 +133,12 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     auto place = [&](const void *p, int64_t step, int64_t row) {
         return Place{p, c.steps > 1 ? step : 0, c.rows > 1 ? row : 0};
     };
-    Place px = place(x, c.x_step, c.x_row), pg = place(gate, c.gate_step, c.gate_row);
+    // nor has a gate per value, and what is not read takes no part in how the columns are shared out
+    Place px = place(x, c.x_step, c.x_row);
+    Place pg = col ? Place{gate, 0, 0} : place(gate, c.gate_step, c.gate_row);
     Place py = place(y, c.y_step, c.y_row), pdy = place(dy, c.dy_step, c.dy_row);
     Place po = back ? place(out, c.dx_step, c.dx_row) : place(out, c.y_step, c.y_row);
-    Place pdg = place(dgate, c.dgate_step, c.dgate_row);
+    Place pdg = col ? Place{dgate, 0, 0} : place(dgate, c.dgate_step, c.dgate_row);
     Place pc = place(cut, c.cut_step, c.cut_row);
     for (const Place *a : {&px, &pg, &py, &pdy, &po, &pdg, &pc})
         if (a->p && (!reachable(a->step, c.steps) || !reachable(a->row, c.rows)))
@@ -146,7 +148,8 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
         return bad("strides of dgate overlap its elements");
     const size_t size = size_of(c.dtype);
     const bool reads_x = !back || gated;
-    const void *all[] = {reads_x ? x : nullptr, gate, y, dy, out, dgate};
+    if (!reads_x) px = Place{nullptr, 0, 0};
+    const void *all[] = {px.p, gate, y, dy, out, dgate};
     for (const void *p : all)
         if (reinterpret_cast<uintptr_t>(p) % size) return bad("a tensor is not aligned to its type");
     const float *floats[] = {first, h0, final};
