@@ -170,7 +170,8 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     const int64_t span = std::min(rows, 4 * 64 / width + 2);
     bool far = false;
     for (const Place *a : {&px, &pg, &py, &pdy, &po, &pdg, &pc})
-        if (a->p) far = far || span * a->row + width >= (int64_t(1) << 32) / int64_t(size);
+        if (a->p)
+            far = far || span * a->row + width >= (int64_t(1) << 32) / int64_t(a == &pc ? 1 : size);
     if (far && c.steps > kMostFar)
         return bad("%lld steps of rows too far apart: more than %lld are taken only where %lld rows "
                    "lie within 2^32 bytes",

@@ -49,3 +49,12 @@ def test_rows_of_an_input_that_is_not_read():
     assert rc == av.AV_EINVAL and "workspace" in why
     rc, why = backward(steps=MANY, x_row=1 << 31, form=av.AV_SCAN_GATED)
     assert rc == av.AV_EINVAL and "apart" in why
+
+
+def test_rows_of_flags_are_bytes():
+    """Three rows of flags 2^29 bytes apart lie within 2^32 bytes; 2^31 apart they do not."""
+    for call in (forward, backward):
+        rc, why = call(steps=MANY, cut_row=1 << 29)
+        assert rc == av.AV_EINVAL and "workspace" in why, why
+        rc, why = call(steps=MANY, cut_row=1 << 31)
+        assert rc == av.AV_EINVAL and "apart" in why, why
