@@ -487,27 +487,30 @@ __global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs p) {
     if (kBack && kCol && p.part) put_states(p.part, c, sum);
 }
 
-// Sums m rows of `width` floats into one row (to type T): a workgroup takes `lanes` values, its
-// threads share the rows, blockIdx.y takes a run of `run` rows.
+// Sums m rows of `width` floats into one row (to type T): a workgroup takes `lanes` values at a time,
+// its threads share the rows, blockIdx.y takes a run of `run` rows.
 template <typename T>
 __global__ void __launch_bounds__(1024) sum_rows_kernel(const float *src, int64_t m, int64_t run,
                                                         int width, int lanes, T *dst) {
     __shared__ float red[1024];
-    const int d = int(blockIdx.x) * lanes + int(threadIdx.x) % lanes;
     const int part = int(threadIdx.x) / lanes, parts = 1024 / lanes;
     const int64_t r0 = int64_t(blockIdx.y) * run, r1 = min(m, r0 + run);
-    float s = 0.0f;
-    if (d < width) {
+    for (int from = int(blockIdx.x) * lanes; from < width; from += int(gridDim.x) * lanes) {
+        const int d = from + int(threadIdx.x) % lanes;
+        float s = 0.0f;
+        if (d < width) {
 #pragma unroll 4
-        for (int64_t r = r0 + part; r < r1; r += parts) s += src[r * width + d];
-    }
-    red[threadIdx.x] = s;
-    __syncthreads();
-    for (int half = parts / 2; half > 0; half >>= 1) {
-        if (part < half) red[threadIdx.x] += red[threadIdx.x + half * lanes];
+            for (int64_t r = r0 + part; r < r1; r += parts) s += src[r * width + d];
+        }
+        red[threadIdx.x] = s;
         __syncthreads();
+        for (int half = parts / 2; half > 0; half >>= 1) {
+            if (part < half) red[threadIdx.x] += red[threadIdx.x + half * lanes];
+            __syncthreads();
+        }
+        if (part == 0 && d < width)
+            dst[int64_t(blockIdx.y) * width + d] = from_f32<T>(red[threadIdx.x]);
     }
-    if (part == 0 && d < width) dst[int64_t(blockIdx.y) * width + d] = from_f32<T>(red[threadIdx.x]);
 }
 
 __global__ void __launch_bounds__(256) copy_state_kernel(const float *src, float *dst, int n) {
@@ -583,7 +586,8 @@ hipError_t run(const ScanArgs &a, const ScanPlan &plan, bool gated, bool col, bo
     const int D = int(a.width);
     int lanes = 1;
     while (lanes < 16 && lanes < D) lanes *= 2;
-    const unsigned blocks = unsigned((D + lanes - 1) / lanes);
+    // a launch has fewer than 2^32 threads, 1024 a workgroup: very wide sums loop
+    const unsigned blocks = unsigned(std::min((D + lanes - 1) / lanes, 1 << 20));
     const float *src = a.part;
     int64_t rows = m;
     if (a.runs > 1) {
