@@ -542,7 +542,8 @@ av_status av_log_probs(const av_tokens_config *cfg, const void *logits, const vo
  * stats and entropy as av_log_probs stored them for the same logits; dlogp, dentropy device float
  * [N], either may be NULL (0; entropy is read only with dentropy, ids only with dlogp).  dlogits:
  * device, dtype, row r at r * drow_stride; may be the logits themselves (the same pointer and
- * stride).  Masked choices and rows without any choice get 0; a row with NaN results gets NaN. */
+ * stride).  Masked choices and rows without any choice get 0, whatever dlogp and dentropy are there (NaN
+ * and infinities included); a row with NaN results gets NaN. */
 av_status av_log_probs_backward(const av_tokens_config *cfg, const void *logits, const void *ids,
                                 const float *stats, const float *entropy, const float *dlogp,
                                 const float *dentropy, void *dlogits);
