@@ -470,8 +470,10 @@ av_status av_scan_workspace(const av_scan_config *cfg, int32_t backward, size_t 
  * is a recurrent agent's memory that starts anew with every episode; T = 1 is its acting step.
  *   x, gate   device, dtype;  cut device uint8 [T][B] or NULL (never)
  *   h0, last  device float [B][D] or NULL: the state before the first step and after the last
- *             processed one (T = 0: h0).  They may be the same buffer.
- *   y         device, dtype; may be x itself (the same pointer and strides)
+ *             processed one (T = 0: h0).  They may be the same buffer, but av_scan_backward takes h0
+ *             as av_scan read it: where a gradient follows, last needs a buffer of its own.
+ *   y         device, dtype; may be x itself (the same pointer and strides), if no gradient of the
+ *             gated form follows, which reads x
  * Products of gates are formed over spans of steps: gates are decays, |a| <= 1 (larger ones work
  * while their product over any span is finite in 32 bits; one below the smallest number in 32 bits
  * counts as 0).  A state that is not finite leaves every
@@ -487,9 +489,11 @@ av_status av_scan(const av_scan_config *cfg, const void *x, const void *gate, co
 
 /* Gradients of av_scan.  dy: the gradient of y (device, dtype); dlast: of last (device float
  * [B][D]) or NULL (0).  y is the output of av_scan, which stands for the states (with a 16-bit
- * type dgate sees them rounded to it).  Outputs: dx (dtype), dgate (dtype; [T][B][D], or [D]
- * summed in 32 bits over T and B, in a fixed order) or NULL if not wanted, dh0 (device float [B][D])
- * or NULL.  x may be NULL in the linear form, which does not read it.  dx may be dy, and dgate
+ * type dgate sees them rounded to it: in the gated form, which takes the difference of state and x, it is
+ * off by up to half a step of the state times lam a (1 - a), lam the gradient of the state).  x, gate, cut
+ * and h0 as av_scan read them (h0 NULL: 0, as there).  Outputs: dx (dtype), dgate (dtype; [T][B][D],
+ * or [D] summed in 32 bits over T and B, in a fixed order) or NULL if not wanted, dh0 (device float
+ * [B][D]) or NULL.  x may be NULL in the linear form, which does not read it.  dx may be dy, and dgate
  * [T][B][D] may be gate (the same pointer and strides); no other output may overlap an input.
  * Workspace and errors as av_scan, with av_scan_workspace(cfg, 1, ...). */
 av_status av_scan_backward(const av_scan_config *cfg, const void *x, const void *gate,

@@ -550,7 +550,8 @@ def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=Fal
             workspace=None):
     """Gated linear recurrence over time.  x, y: device tensors [T][B][D] of one floating type;
     gate the same, or [D]; h0, last: float32 [B][D] or None; cut: uint8 [T][B] or None (a step
-    whose flag is set starts anew).  y may be x.  Runs on the current stream of x's device."""
+    whose flag is set starts anew).  y may be x, and last may be h0, if no gradient follows that reads
+    them.  Runs on the current stream of x's device."""
     lib = load_library()
     kind, form, px, sx, pg, sg, per_value, pc, sc = _scan_common(x, gate, cut, form)
     shape, device = x.shape, x.device
@@ -567,8 +568,8 @@ def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=Fal
 
 def av_scan_backward(x, gate, y, dy, dx, dgate=None, h0=None, dlast=None, dh0=None, cut=None,
                      form="linear", reverse=False, workspace=None):
-    """Gradients of av_scan, called as it was: y its output, dy and dlast the gradients of y and
-    last; dx, dgate (like gate, or None) and dh0 (float32 [B][D], or None) are written."""
+    """Gradients of av_scan, called as it was (h0 with the values it had then): y its output, dy and
+    dlast the gradients of y and last; dx, dgate (like gate, or None) and dh0 (float32 [B][D], or None) are written."""
     lib = load_library()
     kind, form, px, sx, pg, sg, per_value, pc, sc = _scan_common(x, gate, cut, form)
     shape, device, dtype = x.shape, x.device, x.dtype
