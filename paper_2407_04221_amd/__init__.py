@@ -438,6 +438,10 @@ def av_destroy_batch(batch):
 
 
 # --- the learner's operators ----------------------------------------------------------------
+#
+# They read and write the given buffers, and torch's differentiation sees none of it: outputs carry no
+# history and no version is counted.  A gradient is asked for (av_scan_backward,
+# av_log_probs_backward) and handed on, as in logits.backward(dlogits).
 
 # A call's host time is most of a small operator's cost, so arguments are checked with as few steps as
 # will do and its config struct is packed in one (the fields of av_scan_config, av_tokens_config).
@@ -548,7 +552,8 @@ def av_scan_workspace(steps, rows, width, gate_per_value=False, backward=False, 
 
 def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=False,
             workspace=None):
-    """Gated linear recurrence over time.  x, y: device tensors [T][B][D] of one floating type;
+    """Gated linear recurrence over time.  x, y: device tensors [T][B][D] of one floating type, B and D
+    at least 1;
     gate the same, or [D]; h0, last: float32 [B][D] or None; cut: uint8 [T][B] or None (a step
     whose flag is set starts anew).  y may be x, and last may be h0, if no gradient follows that reads
     them.  Runs on the current stream of x's device."""
@@ -767,7 +772,8 @@ class Batch:
 
     def act(self, logits, uniform, actions=None, logp=None):
         """Draw every environment's action for the next step: logits [B][A] and uniform numbers
-        float32 [B] on the device; returns (actions uint8 [B], their log-probabilities [B])."""
+        float32 [B] on the device; returns (actions uint8 [B], their log-probabilities [B], which
+        carry no history of torch's).  Runs on torch's current stream."""
         torch = _torch()
         if tuple(logits.shape[:1]) != (self.B,):
             raise ValueError(f"logits must have {self.B} rows, got {tuple(logits.shape)}")
@@ -780,9 +786,10 @@ class Batch:
 
     def returns(self, rewards, done, gamma, after=None, out=None):
         """Discounted returns of a rollout: rewards float32 [k][B] (or temporal-difference errors,
-        for advantages) and done [k][B] as step_n gives them, gamma a number or a float32 device
-        tensor [1], after float32 [B] the value of what follows the last step (or None); returns
-        out [k][B], out[t] = rewards[t] + gamma (1 - done[t]) out[t + 1]."""
+        for advantages) and done [k][B] as step_n gives them, gamma a float32 device tensor [1] or a
+        number (which every call copies into one), after float32 [B] the value of what follows the
+        last step (or None); returns out [k][B], out[t] = rewards[t] + gamma (1 - done[t]) out[t + 1].
+        Runs on torch's current stream."""
         torch = _torch()
         if rewards.dim() != 2 or rewards.shape[1] != self.B:
             raise ValueError(f"rewards must be [k][{self.B}], got {tuple(rewards.shape)}")
