@@ -26,17 +26,18 @@ template <> __device__ inline bf16_t from_f32<bf16_t>(float v) {
 }
 
 // V neighbouring elements.  Global memory takes an access of up to 16 bytes at any address, so one
-// of V elements needs no more alignment than its element's.
+// of V elements needs no more alignment than its element's.  The words stand for elements of any type, and
+// for smaller words at the same place (a row's last, an output over its input): may_alias says so.
 template <typename T, int V> struct Word { T v[V]; };
 typedef uint64_t Any2 __attribute__((ext_vector_type(2)));
 typedef uint64_t Any4 __attribute__((ext_vector_type(4)));
 template <int kBytes> struct Bits;
 template <> struct Bits<1> { typedef uint8_t type; };
-template <> struct Bits<2> { typedef uint16_t type __attribute__((aligned(1))); };
-template <> struct Bits<4> { typedef uint32_t type __attribute__((aligned(1))); };
-template <> struct Bits<8> { typedef uint64_t type __attribute__((aligned(1))); };
-template <> struct Bits<16> { typedef Any2 type __attribute__((aligned(1))); };
-template <> struct Bits<32> { typedef Any4 type __attribute__((aligned(1))); };    // two accesses
+template <> struct Bits<2> { typedef uint16_t type __attribute__((aligned(1), may_alias)); };
+template <> struct Bits<4> { typedef uint32_t type __attribute__((aligned(1), may_alias)); };
+template <> struct Bits<8> { typedef uint64_t type __attribute__((aligned(1), may_alias)); };
+template <> struct Bits<16> { typedef Any2 type __attribute__((aligned(1), may_alias)); };
+template <> struct Bits<32> { typedef Any4 type __attribute__((aligned(1), may_alias)); };    // two accesses
 
 template <typename E> __device__ inline E load_any(const void *p) {
     const typename Bits<sizeof(E)>::type u =
