@@ -488,14 +488,16 @@ av_status av_scan(const av_scan_config *cfg, const void *x, const void *gate, co
                   size_t workspace_bytes);
 
 /* Gradients of av_scan.  dy: the gradient of y (device, dtype); dlast: of last (device float
- * [B][D]) or NULL (0).  y is the output of av_scan, which stands for the states (with a 16-bit
- * type dgate sees them rounded to it: in the gated form, which takes the difference of state and x, it is
- * off by up to half a step of the state times lam a (1 - a), lam the gradient of the state).  x, gate, cut
- * and h0 as av_scan read them (h0 NULL: 0, as there).  Outputs: dx (dtype), dgate (dtype; [T][B][D],
- * or [D] summed in 32 bits over T and B, in a fixed order) or NULL if not wanted, dh0 (device float
- * [B][D]) or NULL.  x may be NULL in the linear form, which does not read it.  dx may be dy, and dgate
- * [T][B][D] may be gate (the same pointer and strides); no other output may overlap an input.
- * Workspace and errors as av_scan, with av_scan_workspace(cfg, 1, ...). */
+ * [B][D]) or NULL (0).  x, gate, cut and h0 as av_scan read them (h0 NULL: 0, as there), y as it wrote
+ * it.  The states between the steps, which dgate needs, are held in 32 bits: of float they are y itself;
+ * of a 16-bit type they are worked out again from x, gate, cut and h0, and y is not read.
+ * Outputs: dx (dtype), dgate (dtype; [T][B][D], or [D] summed in 32 bits over T and B, in a fixed
+ * order) or NULL if not wanted, dh0 (device float [B][D]) or NULL.  The linear form can do without
+ * x: NULL, or y's pointer where y was written over x.  Then (and always of float) y stands for the
+ * states: a 16-bit y has them rounded, and dgate is off by up to half a step of each times the
+ * gradient of the next state.
+ * dx may be dy, and dgate [T][B][D] may be gate (the same pointer and strides); no other output may
+ * overlap an input.  Workspace and errors as av_scan, with av_scan_workspace(cfg, 1, ...). */
 av_status av_scan_backward(const av_scan_config *cfg, const void *x, const void *gate,
                            const uint8_t *cut, const float *h0, const void *y, const void *dy,
                            const float *dlast, void *dx, void *dgate, float *dh0,

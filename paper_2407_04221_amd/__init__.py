@@ -573,8 +573,8 @@ def av_scan(x, gate, y, h0=None, last=None, cut=None, form="linear", reverse=Fal
 
 def av_scan_backward(x, gate, y, dy, dx, dgate=None, h0=None, dlast=None, dh0=None, cut=None,
                      form="linear", reverse=False, workspace=None):
-    """Gradients of av_scan, called as it was (h0 with the values it had then): y its output, dy and
-    dlast the gradients of y and last; dx, dgate (like gate, or None) and dh0 (float32 [B][D], or None) are written."""
+    """Gradients of av_scan, called as it was (x, gate, cut and h0 with the values they had then; x is y
+    where a linear one was written over x): y its output, dy and dlast the gradients of y and last; dx, dgate (like gate, or None) and dh0 (float32 [B][D], or None) are written."""
     lib = load_library()
     kind, form, px, sx, pg, sg, per_value, pc, sc = _scan_common(x, gate, cut, form)
     shape, device, dtype = x.shape, x.device, x.dtype

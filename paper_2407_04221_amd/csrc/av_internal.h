@@ -315,7 +315,9 @@ struct ScanArgs {
     float *final;
     void *out, *dgate;                // y, or dx; and the gradient of the gates
     float *part;                      // a gate per value: the workgroups' sums
+    bool again;                       // gradient: the states are worked out again, not read from y
     void *slots;                      // chunks > 1: [chunks][N] spans
+    void *state_slots, *marks;        // again: the same of the states; and what leads to each tile
     int64_t x_step, x_row, gate_step, gate_row, y_step, y_row, dy_step, dy_row, out_step, out_row,
         dgate_step, dgate_row, cut_step, cut_row;
 };
@@ -324,12 +326,13 @@ struct ScanPlan {
                                       // columns through all steps); chunks of time
     int64_t chunk;                    // steps
 };
-ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far);
+ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far, bool again);
 struct ScanSpace {
-    size_t part_off, bytes;           // the sums of a gate per value, and all of the workspace
-    int runs;
+    size_t states_off, marks_off, part_off, bytes;   // slots of the states, marks, sums of a gate per
+    int runs;                                        // value, and all of the workspace
+    bool marks;
 };
-ScanSpace scan_space(const ScanPlan &plan, int64_t N, int64_t width, bool sums);
+ScanSpace scan_space(const ScanPlan &plan, int64_t T, int64_t N, int64_t width, bool sums, bool again);
 hipError_t launch_scan(const ScanArgs &a, const ScanPlan &plan, int dtype, bool gated, bool col,
                        bool back, hipStream_t s);
 

@@ -111,15 +111,22 @@ av_status check_workspace(const void *workspace, size_t bytes, size_t needed) {
     return AV_OK;
 }
 
-// The most that any layout of these sizes takes: rows apart, or as one, or far apart.
+// The most that any layout of these sizes takes: rows apart, or as one, or far apart (some, and not too
+// many steps); and, in a gradient of a 16-bit type, with the states worked out again or not.
 size_t workspace_of(const av_scan_config &c, bool back) {
     const int64_t N = c.rows * c.width;
     const bool sums = back && c.gate_per_value;
     size_t most = 0;
-    for (const ScanPlan &plan : {scan_plan(c.steps, c.rows, c.width, c.dtype, false),
-                                 scan_plan(c.steps, 1, N, c.dtype, false),
-                                 scan_plan(c.steps, c.rows, c.width, c.dtype, true)})
-        most = std::max(most, scan_space(plan, N, c.width, sums).bytes);
+    for (const bool again : {false, true}) {
+        if (again && !(back && c.dtype != AV_F32)) break;
+        auto take = [&](int64_t rows, int64_t width, bool far) {
+            const ScanPlan plan = scan_plan(c.steps, rows, width, c.dtype, far, again);
+            most = std::max(most, scan_space(plan, c.steps, N, c.width, sums, again).bytes);
+        };
+        take(c.rows, c.width, false);
+        take(1, N, false);
+        if (c.rows > 1 && c.steps <= kMostFar) take(c.rows, c.width, true);
+    }
     return most;
 }
 
@@ -147,7 +154,9 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     if (back && dgate && !col && !spread(pdg.step, pdg.row, c))
         return bad("strides of dgate overlap its elements");
     const size_t size = size_of(c.dtype);
-    const bool reads_x = !back || gated;
+    // a 16-bit gradient works the states out again, unless x has become y, or is not there
+    const bool again = back && size == 2 && x && (gated || x != y);
+    const bool reads_x = !back || gated || again;
     if (!reads_x) px = Place{nullptr, 0, 0};
     const void *all[] = {px.p, gate, y, dy, out, dgate};
     for (const void *p : all)
@@ -176,8 +185,8 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
         return bad("%lld steps of rows too far apart: more than %lld are taken only where %lld rows "
                    "lie within 2^32 bytes",
                    (long long)c.steps, (long long)kMostFar, (long long)span);
-    const ScanPlan plan = scan_plan(c.steps, rows, width, c.dtype, far);
-    const ScanSpace space = scan_space(plan, c.rows * c.width, c.width, back && col);
+    const ScanPlan plan = scan_plan(c.steps, rows, width, c.dtype, far, again);
+    const ScanSpace space = scan_space(plan, c.steps, c.rows * c.width, c.width, back && col, again);
     if (some) {
         if (av_status st = check_workspace(workspace, workspace_bytes, workspace_of(c, back)))
             return st;
@@ -207,7 +216,12 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     a.cut = reinterpret_cast<const uint8_t *>(turn(pc.p, pc.step, 1));
     a.cut_step = pc.step; a.cut_row = pc.row;
     a.first = first; a.h0 = h0; a.final = final;
+    a.again = again;
     a.slots = some && plan.chunks > 1 ? workspace : nullptr;
+    if (some && space.marks) {
+        a.state_slots = static_cast<char *>(workspace) + space.states_off;
+        a.marks = static_cast<char *>(workspace) + space.marks_off;
+    }
     a.part = back && col && dgate && some
                  ? reinterpret_cast<float *>(static_cast<char *>(workspace) + space.part_off)
                  : nullptr;

@@ -17,6 +17,13 @@
 //
 // The gradient is the same recurrence run the other way: with lam_t the gradient of s_t and
 // c_t that of s_{t-1} through step t, lam_t = dy_t + c_{t+1} and c_t = a_t lam_t (0 where cut).
+// The gates' gradient takes the states.  In 32 bits they are the outputs y.  A 16-bit y has lost what a sum
+// over many steps, or a difference from x, needs (one gate, 4187 rows of 5 steps in bf16: off by 19
+// times the sum), so there the states are worked out again: marks, the spans from a chunk's first step to
+// each of its tiles, come from a pass over x and the gates (over dy too where time is cut, in place of
+// the chunks' pass), and a tile takes its waves' spans in both directions through LDS, with one barrier
+// still.  One tile needs no marks.  (128 x 1024 x 256 in bf16 both ways: 138 us, with the rounded states
+// 111; 65536 x 2 x 320 in f16: 212 us, 189.)
 //
 // Both directions and both time orders are one code: the host points every tensor at the first
 // processed step and gives its step stride a sign; q counts processed steps.
@@ -137,8 +144,8 @@ struct Lanes {
 
 // K consecutive steps of V columns as they come from memory; kEach: with V flags, one for
 // each column.
-template <typename T, int V, int K, bool kX, bool kGate, bool kBack, bool kEach> struct Raw {
-    Word<T, V> e[K], g[kGate ? K : 1], x[kX ? K : 1], before[kBack ? K : 1];
+template <typename T, int V, int K, bool kX, bool kGate, bool kBefore, bool kEach> struct Raw {
+    Word<T, V> e[K], g[kGate ? K : 1], x[kX ? K : 1], before[kBefore ? K : 1];
     Word<uint8_t, kEach ? V : 1> cut[K];
 };
 
@@ -150,11 +157,17 @@ template <int V, int K, bool kRest, bool kEach> struct Work {
     __device__ bool cut(int k, int v) const { return flags[k].v[kEach ? v : 0] != 0; }
 };
 
-// One direction's view of the tensors.  kBack: e is dy, `before` the state before the step, and x is
-// read only where gated; else e is x.
-template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEach> struct Reader {
-    static constexpr bool kX = kBack && kGated, kRest = kBack && kGated;
-    using In = Raw<T, V, K, kX, !kCol, kBack, kEach>;
+// What of a tile's tensors is read: all, or only what a span of the recurrence that is processed needs, or,
+// in the gradient, a span of the states.
+enum Part { kAll, kSpan, kStates };
+
+// One direction's view of the tensors.  kBack: e is dy and `before` the state before the step, of which
+// kAgain reads none but x; without it x is read only where gated.  Else e is x.
+template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kAgain, bool kEach>
+struct Reader {
+    static constexpr bool kX = kBack && (kGated || kAgain), kRest = kBack && kGated;
+    static constexpr bool kBefore = kBack && !kAgain;
+    using In = Raw<T, V, K, kX, !kCol, kBefore, kEach>;
     using Out = Work<V, K, kRest, kEach>;
     using Values = Word<T, V>;
     using Flags = Word<uint8_t, kEach ? V : 1>;
@@ -183,8 +196,8 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEa
         }
     }
 
-    // Steps q .. q + K - 1; past `end` the last step is read again.  kSpan: only what a span needs.
-    template <bool kSpan> __device__ void load(In &r, int q, int end) const {
+    // Steps q .. q + K - 1; past `end` the last step is read again.
+    template <Part kPart> __device__ void load(In &r, int q, int end) const {
         q = min(q, end - 1);
         // the state before processed step q of the gradient is the output one step on
         Lanes::Cursor pe = e.at(q), pg = g.at(q), px = x.at(q), pc = cut.at(q),
@@ -192,16 +205,16 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEa
         const bool whole = q + K < end;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            r.e[k] = pe.template get<Values>();
+            if (kPart != kStates) r.e[k] = pe.template get<Values>();
             if (!kCol) r.g[k] = pg.template get<Values>();
-            if (kX && !kSpan) r.x[k] = px.template get<Values>();
-            if (kBack && !kSpan) r.before[k] = py.template get<Values>();
+            if (kX && kPart != kSpan) r.x[k] = px.template get<Values>();
+            if (kBefore && kPart == kAll) r.before[k] = py.template get<Values>();
             if (whole || q + k + 1 < end) {
                 pe.next();
                 if (!kCol) pg.next();
                 if (kX) px.next();
             }
-            if (kBack && (whole || q + k + 2 < steps)) py.next();
+            if (kBefore && (whole || q + k + 2 < steps)) py.next();
         }
         if (cuts) {
 #pragma unroll
@@ -216,7 +229,7 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEa
     }
 
     // The first n steps in r in 32 bits; the others become steps that change nothing.
-    __device__ void unpack(const In &r, int n, Out &o) const {
+    __device__ void unpack(In &r, int n, Out &o) const {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             o.flags[k] = r.cut[k];
@@ -243,7 +256,9 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEa
                 for (int v = 0; v < V; ++v) {
                     o.a[k][v] = 1.0f;
                     o.b[k][v] = 0.0f;
+                    if (kRest) o.rest[k][v] = 0.0f;
                 }
+                if (kAgain) r.x[k] = Values{};
             }
         }
     }
@@ -261,18 +276,56 @@ template <typename T, int V, int K, bool kGated, bool kCol, bool kBack, bool kEa
             }
     }
 
+    // What step k of the recurrence adds to its state, for the gradient.
+    static __device__ float taken(const In &r, const Out &o, int k, int v) {
+        const float x = to_f32(r.x[kX ? k : 0].v[v]);
+        return kGated ? o.rest[kRest ? k : 0][v] * x : x;
+    }
+    // The span of the states over these steps, which the gradient holds last step first.
+    static __device__ void states_span(const In &r, const Out &o, float2 (&s)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) s[v] = make_float2(1.0f, 0.0f);
+#pragma unroll
+        for (int k = K - 1; k >= 0; --k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float b = taken(r, o, k, v);
+                s[v].y = o.cut(k, v) ? b : fmaf(o.a[k][v], s[v].y, b);
+                s[v].x = o.cut(k, v) ? __builtin_nanf("") : s[v].x * o.a[k][v];
+            }
+    }
+    // The states before these steps, from the one before the first of them (step K - 1 here), which is
+    // taken through all.
+    static __device__ void states(const In &r, const Out &o, float (&s)[V], float (&came)[K][V]) {
+#pragma unroll
+        for (int k = K - 1; k >= 0; --k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float b = taken(r, o, k, v);
+                came[k][v] = o.cut(k, v) ? 0.0f : s[v];
+                s[v] = o.cut(k, v) ? b : fmaf(o.a[k][v], s[v], b);
+            }
+    }
+
     // Takes V states through step k: the output, and the gradient of the gate.  first: this is the
-    // recurrence's first step (the gradient's last), whose state before is h.
+    // recurrence's first step (the gradient's last), whose state before is h; or came holds those of
+    // all steps.
     static __device__ void step(const In &r, const Out &o, int k, bool first, const Word<float, V> &h,
-                                float (&state)[V], float (&out)[V], float (&dgate)[V]) {
+                                const float (&came)[kAgain ? K : 1][V], float (&state)[V],
+                                float (&out)[V], float (&dgate)[V]) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float a = o.a[k][v];
             if (kBack) {
                 const float lam = o.b[k][v] + state[v];
                 state[v] = o.cut(k, v) ? 0.0f : a * lam;
-                float s = first ? h.v[v] : to_f32(r.before[k].v[v]);
-                s = o.cut(k, v) ? 0.0f : s;
+                float s;
+                if constexpr (kAgain) {
+                    s = came[k][v];
+                } else {
+                    s = first ? h.v[v] : to_f32(r.before[k].v[v]);
+                    s = o.cut(k, v) ? 0.0f : s;
+                }
                 out[v] = kGated ? lam * o.rest[k][v] : lam;
                 // lam (s - x) a (1 - a), or lam s
                 dgate[v] = kGated ? out[v] * a * (s - to_f32(r.x[k].v[v])) : lam * s;
@@ -300,7 +353,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_chunks_kernel(ScanArgs 
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int W = blockDim.x >> 6;
     const Column c = column_of<V>(p, group_of_columns() * 64 + lane);
-    using R = Reader<T, V, K, kGated, kCol, kBack, kEach>;
+    using R = Reader<T, V, K, kGated, kCol, kBack, false, kEach>;
     const R in(p, c, __builtin_amdgcn_readfirstlane(c.b));
     const int begin = int(blockIdx.y) * int(p.chunk), part = int(p.chunk) / W;
     float2 total[V];
@@ -309,11 +362,11 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_chunks_kernel(ScanArgs 
     // the chunk is whole (the last one has no part here) and so is each wave's share of it
     const int from = begin + w * part, to = from + part;
     typename R::In raw;
-    in.template load<true>(raw, from, to);
+    in.template load<kSpan>(raw, from, to);
     for (int q = from; q < to; q += K) {
         typename R::Out work;
         in.unpack(raw, K, work);
-        if (q + K < to) in.template load<true>(raw, q + K, to);
+        if (q + K < to) in.template load<kSpan>(raw, q + K, to);
         float2 s[V];
         R::span(work, s);
 #pragma unroll
@@ -340,7 +393,127 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_chunks_kernel(ScanArgs 
     if (blockIdx.y == 0) put_states(slots, c, start);
 }
 
-template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
+// A span as the composition of `next` after it, and of two spans.
+template <int V> __device__ inline void extend(float2 (&s)[V], const float2 (&next)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = make_float2(next[v].x * s[v].x, follow(next[v], s[v].y));
+}
+
+// First kernel of a gradient that works the states out again.  A workgroup goes through its chunk's tiles in
+// the states' order, from the last to the first: marks[tile] takes the span of the states from the
+// chunk's first step up to that tile.  Where time is cut, slots and state_slots take what scan_chunks_kernel
+// says, of the gradient, and of the states: slot i + 1 the i-th chunk in their order.  Each wave reduces
+// its K steps of a tile; wave 0 composes the waves' spans while the others go on.
+template <typename T, int V, bool kGated, bool kCol, bool kCut, bool kEach>
+__global__ void __launch_bounds__(64 * waves_of(V)) scan_marks_kernel(ScanArgs p) {
+    constexpr int K = steps_of(V), kMost = waves_of(V);
+    __shared__ float2 spans[kCut ? 2 : 1][2][kMost * 64 * V];      // of the states, and of the gradient
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int W = blockDim.x >> 6, tile = W * K;
+    const Column c = column_of<V>(p, group_of_columns() * 64 + lane);
+    using R = Reader<T, V, K, kGated, kCol, true, true, kEach>;
+    const R in(p, c, __builtin_amdgcn_readfirstlane(c.b));
+    const int begin = int(blockIdx.y * uint32_t(p.chunk));
+    const int end = int(min(p.T, begin + p.chunk));
+    // no one asks for the span of the tile that the states reach last, unless there are more chunks
+    const int stop = kCut ? begin : begin + tile;
+    const int tiles = (end - begin + tile - 1) / tile;
+    int at = begin + (tiles - 1) * tile;
+    float2 total[V], back[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) total[v] = back[v] = make_float2(1.0f, 0.0f);
+    float2 *marks = static_cast<float2 *>(p.marks);
+    typename R::In next;
+    auto load = [&](int from) { in.template load<kCut ? kAll : kStates>(next, from + w * K, end); };
+    if (at >= stop) load(at);
+    int par = 0;
+    for (; at >= stop; at -= tile) {
+        const int q = at + w * K, n = max(0, min(K, end - q));
+        typename R::In raw = next;
+        typename R::Out work;
+        in.unpack(raw, n, work);
+        if (at > stop) load(at - tile);
+        float2 s[V], g[V];
+        R::states_span(raw, work, s);
+#pragma unroll
+        for (int v = 0; v < V; ++v) spans[0][par][(w * 64 + lane) * V + v] = s[v];
+        if (kCut) {
+            R::span(work, g);
+#pragma unroll
+            for (int v = 0; v < V; ++v) spans[kCut][par][(w * 64 + lane) * V + v] = g[v];
+        }
+        __syncthreads();
+        if (w == 0) {
+            if (c.live) put_states(marks + int64_t(at / tile) * p.N, c, total);
+            for (int j = W - 1; j >= 0; --j) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) s[v] = spans[0][par][(j * 64 + lane) * V + v];
+                extend(total, s);
+            }
+            if (kCut) {                                // the gradient comes to these steps before the others
+#pragma unroll
+                for (int v = 0; v < V; ++v) g[v] = spans[kCut][par][lane * V + v];
+                for (int j = 1; j < W; ++j) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) s[v] = spans[kCut][par][(j * 64 + lane) * V + v];
+                    extend(g, s);
+                }
+                extend(g, back);
+#pragma unroll
+                for (int v = 0; v < V; ++v) back[v] = g[v];
+            }
+        }
+        par ^= 1;
+    }
+    if (w != 0 || !c.live) return;
+    if (at >= begin) put_states(marks + int64_t(at / tile) * p.N, c, total);
+    if (!kCut) return;
+    const int chunks = int(gridDim.y), chunk = int(blockIdx.y);
+    float2 *slots = static_cast<float2 *>(p.slots), *states = static_cast<float2 *>(p.state_slots);
+    float2 start[V];
+    if (chunk + 1 < chunks) put_states(slots + int64_t(chunk + 1) * p.N, c, back);
+    if (chunk > 0) put_states(states + int64_t(chunks - chunk) * p.N, c, total);
+    if (chunk == 0) {
+        const Word<float, V> first = states_at<V>(p.first, c);
+#pragma unroll
+        for (int v = 0; v < V; ++v) start[v] = make_float2(__builtin_nanf(""), first.v[v]);
+        put_states(slots, c, start);
+    }
+    if (chunk + 1 == chunks) {
+        const Word<float, V> h = states_at<V>(p.h0, c);
+#pragma unroll
+        for (int v = 0; v < V; ++v) start[v] = make_float2(__builtin_nanf(""), h.v[v]);
+        put_states(states, c, start);
+    }
+}
+
+// The state that `have` slots lead to: each wave composes its share of them, all waves the shares.
+template <int V>
+__device__ inline void state_after(const void *of, int have, int64_t N, const Column &c, int w, int W,
+                                   float2 *shares, float (&state)[V]) {
+    const float2 *slots = static_cast<const float2 *>(of);
+    const int lane = threadIdx.x & 63, share = (have + W - 1) / W;
+    float2 s[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = make_float2(1.0f, 0.0f);
+    for (int j = w * share; j < min(have, (w + 1) * share); ++j) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float2 one = slots[int64_t(j) * N + c.n + v];
+            s[v] = make_float2(one.x * s[v].x, follow(one, s[v].y));
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) shares[(w * 64 + lane) * V + v] = s[v];
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) state[v] = 0.0f;
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) state[v] = follow(shares[(j * 64 + lane) * V + v], state[v]);
+}
+
+template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kAgain, bool kEach>
 __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     constexpr int K = steps_of(V), kMost = waves_of(V);
     // Loading a tile ahead pays where few workgroups share a compute unit; with many it only
@@ -348,46 +521,33 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     constexpr bool kAhead = V == 1 || !kBack;
     __shared__ float2 spans[2][kMost * 64 * V];
     __shared__ float carry[2][64 * V];        // the state after a tile, for the next one
+    __shared__ float2 state_spans[kAgain ? 2 : 1][kAgain ? kMost * 64 * V : 1];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int W = blockDim.x >> 6;
     const Column c = column_of<V>(p, group_of_columns() * 64 + lane);
-    using R = Reader<T, V, K, kGated, kCol, kBack, kEach>;
+    using R = Reader<T, V, K, kGated, kCol, kBack, kAgain, kEach>;
     const uint32_t b0 = __builtin_amdgcn_readfirstlane(c.b);
     const R in(p, c, b0);
-    // fewer than 2^31 steps: kMost K more do not pass 32 bits unsigned
+    // at most 2^30 steps: kMost K more do not pass 31 bits
     const int begin = int(blockIdx.y * uint32_t(p.chunk));
     const int end = int(min(p.T, begin + p.chunk)), tile = W * K;
     typename R::In next;
-    if (kAhead) in.template load<false>(next, begin + w * K, end);
+    if (kAhead) in.template load<kAll>(next, begin + w * K, end);
     const Word<float, V> h = states_at<V>(kBack ? p.h0 : nullptr, c);
     float state[V];
     int par = 0;
+    float reach[V];                           // the state that the recurrence brings to this chunk
     if (p.slots) {
-        // the chunks before this one: each wave composes its share of them, all waves the shares
-        const float2 *slots = static_cast<const float2 *>(p.slots);
-        const int have = int(blockIdx.y) + 1, share = (have + W - 1) / W;
-        float2 s[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) s[v] = make_float2(1.0f, 0.0f);
-        for (int j = w * share; j < min(have, (w + 1) * share); ++j) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float2 one = slots[int64_t(j) * p.N + c.n + v];
-                s[v] = make_float2(one.x * s[v].x, follow(one, s[v].y));
-            }
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) spans[1][(w * 64 + lane) * V + v] = s[v];
-        __syncthreads();
-#pragma unroll
-        for (int v = 0; v < V; ++v) state[v] = 0.0f;
-        for (int j = 0; j < W; ++j)
-#pragma unroll
-            for (int v = 0; v < V; ++v) state[v] = follow(spans[1][(j * 64 + lane) * V + v], state[v]);
+        state_after(p.slots, int(blockIdx.y) + 1, p.N, c, w, W, spans[1], state);
+        if constexpr (kAgain)
+            state_after(p.state_slots, int(gridDim.y - blockIdx.y), p.N, c, w, W, state_spans[1], reach);
     } else {
         const Word<float, V> first = states_at<V>(p.first, c);
 #pragma unroll
-        for (int v = 0; v < V; ++v) state[v] = first.v[v];
+        for (int v = 0; v < V; ++v) {
+            state[v] = first.v[v];
+            reach[v] = h.v[v];
+        }
     }
     const Lanes out(p.out, p.out_step, p.out_row, sizeof(T), b0, c);
     const Lanes dgate(p.dgate, p.dgate_step, p.dgate_row, sizeof(T), b0, c);
@@ -396,17 +556,33 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     for (int at = begin; at < end; at += tile) {
         const int q = at + w * K;
         const int n = max(0, min(K, end - q));                          // this wave's steps
-        if (!kAhead) in.template load<false>(next, q, end);
-        const typename R::In raw = next;
+        if (!kAhead) in.template load<kAll>(next, q, end);
+        float s0[V];                          // the state before this tile's steps, then this wave's
+        if constexpr (kAgain) {
+            Word<float2, V> mark;
+#pragma unroll
+            for (int v = 0; v < V; ++v) mark.v[v] = make_float2(1.0f, 0.0f);
+            if (p.marks)
+                mark = load_any<Word<float2, V>>(static_cast<const float2 *>(p.marks) +
+                                                 int64_t(at / tile) * p.N + c.n);
+#pragma unroll
+            for (int v = 0; v < V; ++v) s0[v] = follow(mark.v[v], reach[v]);
+        }
+        typename R::In raw = next;
         typename R::Out work;
         in.unpack(raw, n, work);
         // the next tile is on its way while this one is worked on
-        if (kAhead && at + tile < end) in.template load<false>(next, q + tile, end);
+        if (kAhead && at + tile < end) in.template load<kAll>(next, q + tile, end);
         if (W > 1) {
             float2 s[V];
             R::span(work, s);
 #pragma unroll
             for (int v = 0; v < V; ++v) spans[par][(w * 64 + lane) * V + v] = s[v];
+            if constexpr (kAgain) {
+                R::states_span(raw, work, s);
+#pragma unroll
+                for (int v = 0; v < V; ++v) state_spans[par][(w * 64 + lane) * V + v] = s[v];
+            }
             __syncthreads();
             // from the state before the tile through the waves before this one
             if (at > begin) {
@@ -418,13 +594,22 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
 #pragma unroll
                 for (int v = 0; v < V; ++v)
                     state[v] = follow(spans[par][(j * 64 + lane) * V + v], state[v]);
+            if constexpr (kAgain) {
+#pragma unroll 4
+                for (int j = W - 1; j > w; --j)
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        s0[v] = follow(state_spans[par][(j * 64 + lane) * V + v], s0[v]);
+            }
             par ^= 1;
         }
+        float came[kAgain ? K : 1][V];
+        if constexpr (kAgain) R::states(raw, work, s0, came);
         Lanes::Cursor po = out.at(q), pg = dgate.at(q);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             float o[V], dg[V];
-            R::step(raw, work, k, q + k == in.steps - 1, h, state, o, dg);
+            R::step(raw, work, k, q + k == in.steps - 1, h, came, state, o, dg);
             if (k < n) {                      // the others change nothing and are no one's output
                 if (c.live) po.put(rounded<T, V>(o), c);
                 if (with_gate && c.live) pg.put(rounded<T, V>(dg), c);
@@ -459,29 +644,67 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
 }
 
 // A few steps (an agent's acting step is one): a lane takes its columns through all of them.  Its
-// addresses are 64 bits a lane, so any distance between rows will do.
-template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
+// addresses are 64 bits a lane, so any distance between rows will do.  The states are worked out again for
+// four steps at a time, from h0 or, of more than 32 steps (rows far apart), from the state at the next
+// border of 32, which a first pass leaves in the workspace.
+constexpr int kShortSteps = 4, kShortMark = 32;
+template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kAgain, bool kEach>
 __global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs p) {
+    constexpr int K = kAgain ? kShortSteps : 1;
     const Column c = column_of<V>(p, int64_t(blockIdx.x) * 256 + threadIdx.x);
     if (!c.live) return;
-    using R = Reader<T, V, 1, kGated, kCol, kBack, kEach>;
+    using R = Reader<T, V, K, kGated, kCol, kBack, kAgain, kEach>;
     const R in(p, c, c.b);
     const Word<float, V> h = states_at<V>(kBack ? p.h0 : nullptr, c);
     Word<float, V> state = states_at<V>(p.first, c);
     const Lanes out(p.out, p.out_step, p.out_row, sizeof(T), c.b, c);
     const Lanes dgate(p.dgate, p.dgate_step, p.dgate_row, sizeof(T), c.b, c);
     float sum[V] = {};
-    for (int q = 0; q < in.steps; ++q) {
-        typename R::In raw;
-        typename R::Out work;
-        in.template load<false>(raw, q, p.T);
-        in.unpack(raw, 1, work);
-        float o[V], dg[V];
-        R::step(raw, work, 0, q == in.steps - 1, h, state.v, o, dg);
-        out.at(q).put(rounded<T, V>(o), c);
-        if (kBack && !kCol && p.dgate) dgate.at(q).put(rounded<T, V>(dg), c);
+    typename R::In raw;
+    typename R::Out work;
+    float came[kAgain ? K : 1][V];
+    const int last = (in.steps - 1) / K * K;           // where the recurrence's first steps are
+    float *marks = static_cast<float *>(p.marks);
+    // takes the states from before steps from .. from + K - 1 (the recurrence's last of them first) through
+    auto through = [&](int from, Word<float, V> &s) {
+        if constexpr (kAgain) {
+            in.template load<kStates>(raw, from, in.steps);
+            in.unpack(raw, min(K, in.steps - from), work);
+            R::states(raw, work, s.v, came);
+        }
+    };
+    if (kAgain && in.steps > kShortMark) {
+        Word<float, V> s = h;
+        for (int at = last; at >= kShortMark; at -= K) {
+            through(at, s);
+            if (at % kShortMark == 0) put_states(marks + int64_t(at / kShortMark - 1) * p.N, c, s.v);
+        }
+    }
+    for (int at = 0; at < in.steps; at += K) {
+        if constexpr (kAgain) {
+            const int group = at / kShortMark;
+            Word<float, V> s = h;
+            if (group < last / kShortMark)
+                __builtin_memcpy(s.v, marks + int64_t(group) * p.N + c.n, sizeof s.v);
+            for (int f = min(last, (group + 1) * kShortMark - K); f > at; f -= K) through(f, s);
+            in.template load<kAll>(raw, at, in.steps);
+            in.unpack(raw, min(K, in.steps - at), work);
+            R::states(raw, work, s.v, came);
+        } else {
+            in.template load<kAll>(raw, at, in.steps);
+            in.unpack(raw, K, work);
+        }
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += kBack && kCol ? dg[v] : 0.0f;
+        for (int k = 0; k < K; ++k) {
+            const int q = at + k;
+            if (q >= in.steps) break;
+            float o[V], dg[V];
+            R::step(raw, work, k, q == in.steps - 1, h, came, state.v, o, dg);
+            out.at(q).put(rounded<T, V>(o), c);
+            if (kBack && !kCol && p.dgate) dgate.at(q).put(rounded<T, V>(dg), c);
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += kBack && kCol ? dg[v] : 0.0f;
+        }
     }
     if (p.final) put_states(p.final, c, state.v);
     if (kBack && kCol && p.part) put_states(p.part, c, sum);
@@ -533,33 +756,49 @@ unsigned scan_groups(int64_t places) {
     return unsigned(n < 64 ? n : (n + 7) / 8 * 8);
 }
 
-template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kEach>
+template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kAgain, bool kEach>
 hipError_t launch(const ScanArgs &all, const ScanPlan &plan, hipStream_t s) {
     ScanArgs a = all;
     a.lanes = scan_places(1, a.D, V);
     a.places = a.N / a.D * a.lanes;
     if (plan.waves == 0) {
         const unsigned blocks = unsigned((a.places + 255) / 256);
-        hipLaunchKernelGGL((scan_short_kernel<T, V, kGated, kCol, kBack, kEach>), dim3(blocks), dim3(256),
-                           0, s, a);
+        hipLaunchKernelGGL((scan_short_kernel<T, V, kGated, kCol, kBack, kAgain, kEach>), dim3(blocks),
+                           dim3(256), 0, s, a);
         return hipGetLastError();
     }
     const unsigned groups = scan_groups(a.places);
-    if (plan.chunks > 1)
+    const dim3 block(64 * plan.waves);
+    if constexpr (kAgain) {
+        if (plan.chunks > 1)
+            hipLaunchKernelGGL((scan_marks_kernel<T, V, kGated, kCol, true, kEach>),
+                               dim3(groups, plan.chunks), block, 0, s, a);
+        else if (a.marks)
+            hipLaunchKernelGGL((scan_marks_kernel<T, V, kGated, kCol, false, kEach>), dim3(groups),
+                               block, 0, s, a);
+    } else if (plan.chunks > 1) {
         hipLaunchKernelGGL((scan_chunks_kernel<T, V, kGated, kCol, kBack, kEach>),
-                           dim3(groups, plan.chunks - 1), dim3(64 * plan.waves), 0, s, a);
-    hipLaunchKernelGGL((scan_kernel<T, V, kGated, kCol, kBack, kEach>), dim3(groups, plan.chunks),
-                       dim3(64 * plan.waves), 0, s, a);
+                           dim3(groups, plan.chunks - 1), block, 0, s, a);
+    }
+    hipLaunchKernelGGL((scan_kernel<T, V, kGated, kCol, kBack, kAgain, kEach>),
+                       dim3(groups, plan.chunks), block, 0, s, a);
     return hipGetLastError();
 }
 
 template <typename T, int V, bool kGated, bool kEach>
 hipError_t pick(const ScanArgs &a, const ScanPlan &plan, bool col, bool back, hipStream_t s) {
-    if (back)
-        return col ? launch<T, V, kGated, true, true, kEach>(a, plan, s)
-                   : launch<T, V, kGated, false, true, kEach>(a, plan, s);
-    return col ? launch<T, V, kGated, true, false, kEach>(a, plan, s)
-               : launch<T, V, kGated, false, false, kEach>(a, plan, s);
+    if constexpr (sizeof(T) == 2 && V <= 2) {          // the gated form's gradient always has x
+        if (back && (kGated || a.again))
+            return col ? launch<T, V, kGated, true, true, true, kEach>(a, plan, s)
+                       : launch<T, V, kGated, false, true, true, kEach>(a, plan, s);
+    }
+    if constexpr (sizeof(T) == 4 || !kGated) {
+        if (back)
+            return col ? launch<T, V, kGated, true, true, false, kEach>(a, plan, s)
+                       : launch<T, V, kGated, false, true, false, kEach>(a, plan, s);
+    }
+    return col ? launch<T, V, kGated, true, false, false, kEach>(a, plan, s)
+               : launch<T, V, kGated, false, false, false, kEach>(a, plan, s);
 }
 
 template <typename T, int V>
@@ -609,8 +848,9 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 
 // How the sizes are shared out.  B rows of D values, all rows as one where they lie one behind the
 // other; far: rows too far apart for a wave's addressing.
-//   A lane takes a word of columns of up to 8 bytes, as long as that leaves at most a fifth of
-//   the lanes' columns to no one.  Odd widths too in 16 bits (30230 x 325 in bf16 both ways: 94 us,
+//   A lane takes a word of columns of up to 8 bytes, in a gradient that works the states out again of up to
+//   4 (128 x 1024 x 256 in bf16: 76 us, with 8 it needs 160 registers and 87 us), as long as that leaves
+//   at most a fifth of the lanes' columns to no one.  Odd widths too in 16 bits (30230 x 325 in bf16 both ways: 94 us,
 //   with single columns 109), but not in 32 (777 x 33 x 129: 42 us, with single columns 39).
 //   A few steps, or far rows: a lane takes its columns through all of them.
 //   Else words where they still fill the device, for their longer row segments (128 x 1024 x 256 in
@@ -625,11 +865,11 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 //   uncut recurrence's tiles evenly (300 x 16384 in f32: 14.4 us, so 13.5; 140 x 500 x 40: 11.6, so
 //   11.0), but with words, where memory is the bound, only if that drops more than a quarter (40 x
 //   1024 x 256 in f32: 27.5 us, so 23.9; but 80 x 8192 x 64 in f16, a quarter less: 58.4, so 59.3).
-ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far) {
+ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far, bool again) {
     ScanPlan plan{};
     plan.chunks = 1;
     plan.chunk = std::max<int64_t>(1, T);
-    plan.vec = dtype == AV_F32 ? 2 : 4;
+    plan.vec = dtype == AV_F32 || again ? 2 : 4;
     while (plan.vec > 1 && (plan.vec > D || scan_places(1, D, plan.vec) * plan.vec * 4 > D * 5 ||
                             (dtype == AV_F32 && D % plan.vec)))
         plan.vec /= 2;
@@ -657,11 +897,26 @@ ScanPlan scan_plan(int64_t T, int64_t B, int64_t D, int dtype, bool far) {
     return plan;
 }
 
-// The workspace of a plan: the chunks' spans, then, for a gradient of `width` gates, the sums of them
-// that the workgroups leave: one row of `width` for each chunk and row of the recurrence.
-ScanSpace scan_space(const ScanPlan &plan, int64_t N, int64_t width, bool sums) {
-    ScanSpace space{0, 0, 1};
-    if (plan.chunks > 1) space.bytes = round16(size_t(plan.chunks) * size_t(N) * sizeof(float2));
+// The workspace of a plan: the chunks' spans, of the states too where they are worked out again, then the
+// marks of each tile (or a lane's states at its borders), then, for a gradient of `width` gates, the sums of
+// them that the workgroups leave: one row of `width` for each chunk and row of the recurrence.
+ScanSpace scan_space(const ScanPlan &plan, int64_t T, int64_t N, int64_t width, bool sums, bool again) {
+    ScanSpace space{0, 0, 0, 0, 1, false};
+    const size_t row = size_t(N) * sizeof(float2);
+    if (plan.chunks > 1) space.bytes = round16(size_t(plan.chunks) * row);
+    space.states_off = space.marks_off = space.bytes;
+    if (again) {
+        if (plan.chunks > 1) space.bytes += round16(size_t(plan.chunks) * row);
+        space.marks_off = space.bytes;
+        if (plan.waves == 0) {
+            const int64_t n = (T + kShortMark - 1) / kShortMark;
+            if (n > 1) space.bytes += round16(size_t(n - 1) * size_t(N) * sizeof(float));
+        } else {
+            const int64_t tile = plan.waves * steps_of(plan.vec), n = (T + tile - 1) / tile;
+            if (n > 1) space.bytes += round16(size_t(n) * row);
+        }
+        space.marks = space.bytes > space.marks_off;
+    }
     space.part_off = space.bytes;
     if (sums) {
         const int64_t m = plan.chunks * (N / width);
