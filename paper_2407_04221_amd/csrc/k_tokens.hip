@@ -8,7 +8,7 @@
 // others are then summed on their own, R = S - 1, so that log2 S = log2 e log1p R keeps the bits that
 // 1 + R drops (logits 0 and four of -16: log p = -4.50e-7, from the sum -4.77e-7), and with it log p
 // and H, which is a sum of two terms that are not negative.  (1638400 rows of 5 in f32, many of them like
-// this, both ways: 29.6 us, without 29.2.)  The difference is taken before the multiplication: l L - m L
+// this, both ways: 29.9 us, without 29.0.)  The difference is taken before the multiplication: l L - m L
 // as one fused operation is shorter, but m L passes the largest number where all logits are the
 // type's lowest.  A masked choice has t = -inf and adds nothing; t is bounded below in the product
 // t 2^t so that its 0 is not -inf x 0.  A NaN or +inf among the logits makes S a NaN.
@@ -120,6 +120,11 @@ __device__ inline bool certain(float s) { return s < 1.5f; }
 __device__ inline float weight_below(float l, float m) {
     return l < m ? exp2_of((l - m) * kLog2e) : 0.0f;
 }
+// A weight, or 0 for the largest's, which rows of one thread or of few lanes sum beside S: one instruction and
+// an addition an element, whatever the logits (300000 x 148 in f32: 29.3 us, without 28; only for rows that need
+// it, 28.7 where none does and 31.4 where many do; x 300 in f16 47, without 40, and 43.6 and 50.7).  One that rounds to 1 is left
+// out too, but then S is not certain().
+__device__ inline float below_one(float e) { return __builtin_amdgcn_fractf(e); }
 
 // log (1 + x) for 0 <= x <= 1/2, twice the area hyperbolic tangent of z = x / (2 + x) <= 1/5: z (1 + z^2 / 3 +
 // .. + z^10 / 11), of which the next term is 3e-10.  Within 4 roundings of itself.
@@ -235,8 +240,7 @@ __global__ void __launch_bounds__(256) small_rows_kernel(TokenArgs a) {
     for (int i = 0; i < kA; ++i) st.m = fmaxf(st.m, v[i]);
 #pragma unroll
     for (int i = 0; i < kA; ++i) {
-        const float e = add(st, v[i]);
-        others += v[i] < st.m ? e : 0.0f;
+        others += below_one(add(st, v[i]));
     }
     const Row r = row_of(st, others);
     put_row(a, r, row, given);
@@ -482,20 +486,14 @@ __global__ void __launch_bounds__(256) team_rows_kernel(TokenArgs a) {
 #pragma unroll
     for (int j = 0; j < kWords; ++j) m = fmaxf(m, largest(v[j]));
     Stat st{team_max<kLanes>(m), 0.0f, 0.0f};
+    float others = 0.0f;
 #pragma unroll
     for (int j = 0; j < kWords; ++j)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) add(st, v[j][i]);
+        for (int i = 0; i < kPer; ++i) others += below_one(add(st, v[j][i]));
     st.s = team_sum<kLanes>(st.s);
     st.w = team_sum<kLanes>(st.w);
-    float others = 0.0f;
-    if (__any(certain(st.s))) {
-#pragma unroll
-        for (int j = 0; j < kWords; ++j)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) others += weight_below(v[j][i], st.m);
-        others = team_sum<kLanes>(others);
-    }
+    others = team_sum<kLanes>(others);
     const Row r = row_of(st, others);
     if (lane == 0 && live) put_row(a, r, row, given);
     if (a.top == 0) return;
@@ -520,6 +518,40 @@ __device__ inline uint64_t kth_of_wave(uint64_t key, int k) {
     const int above = __popcll(__ballot(hi > t)), equal = __popcll(__ballot(hi == t));
     if (t == 0 || above + equal == k) return uint64_t(t) << 32;
     return uint64_t(t) << 32 | kth_of_wave(hi == t ? uint32_t(key) : 0u, k - above);
+}
+
+// Adds a lane's words to its (empty) sums; sums[] takes what each word's weights come to.
+template <int kWords, int kPer>
+__device__ inline void add_words(Stat &st, const float (&v)[kWords][kPer], float (&sums)[kWords]) {
+    float all = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+        st.s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) add(st, v[j][i]);
+        sums[j] = st.s;
+        all += st.s;
+    }
+    st.s = all;
+}
+// A lane's part of S - 1 where S is certain(): one word of one lane has the largest, m, and only its sum has lost
+// bits to the 1, so only its weights are taken again (20000 x 3000 in bf16, logits of deviation 8: 24.8 us,
+// with every word's 28.5; of deviation 2, where no row is certain, 22.8).
+template <int kWords, int kPer>
+__device__ inline float others_of(const float (&v)[kWords][kPer], const float (&sums)[kWords], float m) {
+    float e = 0.0f, x[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = kNone;
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+        const bool here = largest(v[j]) == m;
+        e += here ? 0.0f : sums[j];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] = here ? v[j][i] : x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) e += weight_below(x[i], m);
+    return e;
 }
 
 constexpr int kWaveList = 256;       // candidates for the alternatives of a wave's row
@@ -549,20 +581,12 @@ __global__ void __launch_bounds__(256) wave_rows_kernel(TokenArgs a) {
 #pragma unroll
     for (int j = 0; j < kWords; ++j) m = fmaxf(m, largest(v[j]));
     Stat st{wave_max(m), 0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < kWords; ++j)
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) add(st, v[j][i]);
+    float sums[kWords];
+    add_words(st, v, sums);
     st.s = wave_sum(st.s);
     st.w = wave_sum(st.w);
     float others = 0.0f;
-    if (certain(st.s)) {                                // the same in all lanes
-#pragma unroll
-        for (int j = 0; j < kWords; ++j)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) others += weight_below(v[j][i], st.m);
-        others = wave_sum(others);
-    }
+    if (certain(st.s)) others = wave_sum(others_of(v, sums, st.m));      // the same in all lanes
     const Row r = row_of(st, others);
     if (lane == 0) put_row(a, r, row, given);
     if (a.top == 0) return;
@@ -729,18 +753,26 @@ __device__ void alternatives(const TokenArgs &a, const Parts<T> &in, float m, Pu
     }
 }
 
-// The weights of a row's, or a part's, words below its largest, which all threads name.
+// A row's, or a part's, S - 1, where S is certain() and so one thread has the largest; st the thread's own
+// sums, m the row's largest.  That thread's sum is the one that has lost bits to the 1: its wave takes
+// its words once more, one a lane.
 template <typename T, int kThreads>
-__device__ float others_of(const Parts<T> &in, float m) {
+__device__ float others_of(const Parts<T> &in, const Stat &st, float m) {
     constexpr int kPer = Parts<T>::kPer, kWaves = kThreads / 64;
     __shared__ float sums[kWaves];
-    const int lane = threadIdx.x & 63;
-    float e = 0.0f;
-    for (int word = in.from + threadIdx.x; word < in.to; word += kThreads) {
-        float v[kPer];
-        in.load(word, v);
+    const int lane = threadIdx.x & 63, first = threadIdx.x & ~63;
+    const unsigned long long who = __ballot(st.m == m);
+    Stat up = st;
+    raise(up, m);
+    float e = st.m == m ? 0.0f : up.s;
+    if (who) {
+        const int holder = first + __ffsll(who) - 1;
+        for (int word = in.from + holder + lane * kThreads; word < in.to; word += 64 * kThreads) {
+            float v[kPer];
+            in.load(word, v);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) e += weight_below(v[i], m);
+            for (int i = 0; i < kPer; ++i) e += weight_below(v[i], m);
+        }
     }
     e = wave_sum(e);
     if (lane == 0) sums[threadIdx.x >> 6] = e;
@@ -798,6 +830,7 @@ __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
             }
         }
     }
+    const Stat own = st;
     const float mine = st.m;
     st = join_lanes(st);
     if (lane == 0) stats[w] = st;
@@ -806,7 +839,7 @@ __global__ void __launch_bounds__(kThreads) long_rows_kernel(TokenArgs a) {
     if (lane < kWaves) all = stats[lane];
     all = join_lanes(all);                              // the same in all waves
     float others = all.s - 1.0f;
-    if (certain(all.s)) others = others_of<T, kThreads>(in, all.m);
+    if (certain(all.s)) others = others_of<T, kThreads>(in, own, all.m);
     if (kSplit) {
         const int64_t at = row * a.parts + blockIdx.y;
         if (tid == 0) static_cast<Stat *>(a.part_stats)[at] = Stat{all.m, others, all.w};
