@@ -154,8 +154,9 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     if (back && dgate && !col && !spread(pdg.step, pdg.row, c))
         return bad("strides of dgate overlap its elements");
     const size_t size = size_of(c.dtype);
-    // a 16-bit gradient works the states out again, unless x has become y, or is not there
-    const bool again = back && size == 2 && x && (gated || x != y);
+    // a 16-bit gradient works the states out again, unless x has become y, or is not there, or no one
+    // asks for the gates' gradient (the gated kernels then do without marks)
+    const bool again = back && size == 2 && x && (gated || (x != y && dgate));
     const bool reads_x = !back || gated || again;
     if (!reads_x) px = Place{nullptr, 0, 0};
     const void *all[] = {px.p, gate, y, dy, out, dgate};
@@ -218,7 +219,7 @@ av_status scan(const av_scan_config *cfg, const void *x, const void *gate, const
     a.first = first; a.h0 = h0; a.final = final;
     a.again = again;
     a.slots = some && plan.chunks > 1 ? workspace : nullptr;
-    if (some && space.marks) {
+    if (some && space.marks && (dgate || plan.chunks > 1)) {
         a.state_slots = static_cast<char *>(workspace) + space.states_off;
         a.marks = static_cast<char *>(workspace) + space.marks_off;
     }

@@ -403,7 +403,7 @@ template <int V> __device__ inline void extend(float2 (&s)[V], const float2 (&ne
 
 // First kernel of a gradient that works the states out again.  A workgroup goes through its chunk's tiles in
 // the states' order, from the last to the first: marks[tile] takes the span of the states from the
-// chunk's first step up to that tile.  Where time is cut, slots and state_slots take what scan_chunks_kernel
+// chunk's first step up to that tile (of the chunk's last tile nothing: it starts there).  Where time is cut, slots and state_slots take what scan_chunks_kernel
 // says, of the gradient, and of the states: slot i + 1 the i-th chunk in their order.  Each wave reduces
 // its K steps of a tile; wave 0 composes the waves' spans while the others go on.
 template <typename T, int V, bool kGated, bool kCol, bool kCut, bool kEach>
@@ -420,7 +420,8 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_marks_kernel(ScanArgs p
     // no one asks for the span of the tile that the states reach last, unless there are more chunks
     const int stop = kCut ? begin : begin + tile;
     const int tiles = (end - begin + tile - 1) / tile;
-    int at = begin + (tiles - 1) * tile;
+    const int top = begin + (tiles - 1) * tile;
+    int at = top;
     float2 total[V], back[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) total[v] = back[v] = make_float2(1.0f, 0.0f);
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_marks_kernel(ScanArgs p
         }
         __syncthreads();
         if (w == 0) {
-            if (c.live) put_states(marks + int64_t(at / tile) * p.N, c, total);
+            if (c.live && at < top) put_states(marks + int64_t(at / tile) * p.N, c, total);
             for (int j = W - 1; j >= 0; --j) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) s[v] = spans[0][par][(j * 64 + lane) * V + v];
@@ -468,7 +469,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_marks_kernel(ScanArgs p
         par ^= 1;
     }
     if (w != 0 || !c.live) return;
-    if (at >= begin) put_states(marks + int64_t(at / tile) * p.N, c, total);
+    if (at >= begin && at < top) put_states(marks + int64_t(at / tile) * p.N, c, total);
     if (!kCut) return;
     const int chunks = int(gridDim.y), chunk = int(blockIdx.y);
     float2 *slots = static_cast<float2 *>(p.slots), *states = static_cast<float2 *>(p.state_slots);
@@ -564,7 +565,7 @@ __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
             Word<float2, V> mark;
 #pragma unroll
             for (int v = 0; v < V; ++v) mark.v[v] = make_float2(1.0f, 0.0f);
-            if (p.marks)
+            if (p.marks && at + tile < end)
                 mark = load_any<Word<float2, V>>(static_cast<const float2 *>(p.marks) +
                                                  int64_t(at / tile) * p.N + c.n);
 #pragma unroll
@@ -675,7 +676,7 @@ __global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs p) {
             R::states(raw, work, s.v, came);
         }
     };
-    if (kAgain && in.steps > kShortMark) {
+    if (kAgain && marks) {
         Word<float, V> s = h;
         for (int at = last; at >= kShortMark; at -= K) {
             through(at, s);
@@ -686,7 +687,7 @@ __global__ void __launch_bounds__(256) scan_short_kernel(ScanArgs p) {
         if constexpr (kAgain) {
             const int group = at / kShortMark;
             Word<float, V> s = h;
-            if (group < last / kShortMark)
+            if (marks && group < last / kShortMark)
                 __builtin_memcpy(s.v, marks + int64_t(group) * p.N + c.n, sizeof s.v);
             for (int f = min(last, (group + 1) * kShortMark - K); f > at; f -= K) through(f, s);
             in.template load<kAll>(raw, at, in.steps);
@@ -915,7 +916,7 @@ ScanSpace scan_space(const ScanPlan &plan, int64_t T, int64_t N, int64_t width, 
             if (n > 1) space.bytes += round16(size_t(n - 1) * size_t(N) * sizeof(float));
         } else {
             const int64_t tile = plan.waves * steps_of(plan.vec), n = (T + tile - 1) / tile;
-            if (n > 1) space.bytes += round16(size_t(n) * row);
+            if (n > 1) space.bytes += round16(size_t(plan.chunks > 1 ? n : n - 1) * row);
         }
         space.marks = space.bytes > space.marks_off;
     }

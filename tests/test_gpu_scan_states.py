@@ -158,6 +158,30 @@ def test_linear_over_x():
     ref.check(host(dgate), want["dgate"], "dgate", "f16")
 
 
+@pytest.mark.parametrize("form", ["linear", "gated"])
+@pytest.mark.parametrize("columns", [False, True])
+@pytest.mark.parametrize("T,B,D", [(6, 50, 8), (70, 300, 130), (1500, 2, 12)])
+def test_without_the_gates_gradient(T, B, D, form, columns):
+    """dx and dh0, asked for dgate or not."""
+    r = np.random.default_rng(6)
+    new = lambda *s: torch.from_numpy(r.uniform(-1, 1, size=s)).half().cuda()
+    x, dy, gate = new(T, B, D), new(T, B, D), new(D) if columns else new(T, B, D)
+    cut = torch.from_numpy((r.random((T, B)) < 0.05).astype(np.uint8)).cuda()
+    y = torch.empty_like(x)
+    av.av_scan(x, gate, y, cut=cut, form=form)
+    outs = []
+    for dgate in (torch.empty_like(gate), None):
+        dx, dh0 = torch.empty_like(x), torch.empty((B, D), device="cuda")
+        av.av_scan_backward(x, gate, y, dy, dx, dgate, dh0=dh0, cut=cut, form=form)
+        outs.append((dx, dh0))
+    if form == "gated":                    # the linear one reads y then, in words of other widths
+        assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    want = ref.scan(host(x), host(gate), None, cut.cpu().numpy(), form, dy=host(dy), dtype="f16")
+    for dx, dh0 in outs:
+        ref.check(host(dx), want["dx"], "dx", "f16")
+        ref.check(host(dh0), want["dh0"], "dh0")
+
+
 def test_a_graph_beside_eager_calls():
     T, B, D = 400, 3, 20
     r = np.random.default_rng(5)
