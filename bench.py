@@ -205,7 +205,7 @@ def bench_learn(av, torch, wl, b, acts, stream, width, seed):
     out["memory"] = {"api": "av_scan", **roof(n * (3 * D * 2 + 1), us)}
     us = _time_us(lambda: av.av_scan_backward(x, gate, y, dy, dx, dgate, cut=flags, form="gated"),
                   stream, torch, reps=20)
-    out["memory_gradient"] = {"api": "av_scan_backward", **roof(n * (6 * D * 2 + 1), us)}
+    out["memory_gradient"] = {"api": "av_scan_backward", **roof(n * (5 * D * 2 + 1), us)}
     del x, gate, dy, y, dx, dgate
     logits, ids = normal(n, 5), acts[:k].reshape(n)
     logp, entropy = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")

@@ -36,8 +36,8 @@ namespace av {
 namespace {
 
 // Steps a wave holds, and most waves of a workgroup: a lane with one column holds 8 steps, one with
-// a word of columns 4, which leaves registers for more waves a SIMD (4 columns x 8 steps of the
-// gradient need 183 registers and run at two waves a SIMD).
+// a word of columns 4, which leaves registers for more waves a SIMD (a gradient that works the states out
+// takes 92 for 2 columns x 4 steps, and 160, two waves a SIMD, for 4 x 4).
 constexpr int steps_of(int V) { return V == 1 ? 8 : 4; }
 constexpr int waves_of(int V) { return V == 1 ? 16 : 8; }
 template <typename T> constexpr int kWide = 8 / sizeof(T);      // columns of a lane's 8-byte word
@@ -127,7 +127,7 @@ struct Lanes {
         uint32_t off;
         template <typename E> __device__ E get() const { return load_any<E>(p + off); }
         // Written past the caches: outputs are not read again by the kernel, and the inputs that
-        // other workgroups still want stay (65536 x 2 x 320 in f16 both ways: 188 us, without 202).
+        // other workgroups still want stay (65536 x 2 x 320 in f16 both ways: 210 us, through them 227).
         // c.odd is the same for the wave, so that most waves never look at their lanes' skip.
         template <typename T, int V> __device__ void put(const Word<T, V> &e, const Column &c) const {
             char *to = const_cast<char *>(p) + off;
@@ -520,7 +520,7 @@ template <typename T, int V, bool kGated, bool kCol, bool kBack, bool kAgain, bo
 __global__ void __launch_bounds__(64 * waves_of(V)) scan_kernel(ScanArgs p) {
     constexpr int K = steps_of(V), kMost = waves_of(V);
     // Loading a tile ahead pays where few workgroups share a compute unit; with many it only
-    // costs registers, in the gradient too many (128 x 1024 x 256 in bf16: 92 us, without 80).
+    // costs registers, in the gradient too many (128 x 1024 x 256 in bf16: 81 us, without 76).
     constexpr bool kAhead = V == 1 || !kBack;
     __shared__ float2 spans[2][kMost * 64 * V];
     __shared__ float carry[2][64 * V];        // the state after a tile, for the next one
@@ -853,15 +853,15 @@ size_t round16(size_t n) { return (n + 15) & ~size_t(15); }
 // other; far: rows too far apart for a wave's addressing.
 //   A lane takes a word of columns of up to 8 bytes, in a gradient that works the states out again of up to
 //   4 (128 x 1024 x 256 in bf16: 76 us, with 8 it needs 160 registers and 87 us), as long as that leaves
-//   at most a fifth of the lanes' columns to no one.  Odd widths too in 16 bits (30230 x 325 in bf16 both ways: 94 us,
-//   with single columns 109), but not in 32 (777 x 33 x 129: 42 us, with single columns 39).
+//   at most a fifth of the lanes' columns to no one.  Odd widths too in 16 bits (30230 x 325 in bf16 both ways: 87 us,
+//   with single columns 106), but not in 32 (777 x 33 x 129: 42 us, with single columns 39).
 //   A few steps, or far rows: a lane takes its columns through all of them.
 //   Else words where they still fill the device, for their longer row segments (128 x 1024 x 256 in
 //   bf16: 42 us forward, with single columns 50), and one column where only that does (2048 x 64 x
 //   256: 58 us, with words 151).  Where neither does, and there are more than three tiles of sixteen
 //   waves of single columns (at some 2 us a tile; below that a second launch costs more), time is
 //   cut into chunks, and words are taken again, smaller ones where they leave fewer lanes idle
-//   (65536 x 2 x 320 in f16: 188 us both ways, with the longest 219).
+//   (65536 x 2 x 320 in f16: 210 us both ways, with the longest 223).
 //   Waves: eight, or sixteen where there is at most one uncut workgroup a compute unit, which has to
 //   hide its own latency (1000 x 16384 in f32: 26.3 us, with eight 27.7; but 300 x 500 x 33, some
 //   units with two workgroups: 22.1 with sixteen, 18.4 with eight).  No more of them than share an

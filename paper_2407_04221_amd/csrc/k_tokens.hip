@@ -35,8 +35,8 @@ constexpr int kTeamBack = 256;
 // Words of all rows from which few lanes take a row, with several words each: fewer reductions and row
 // results an instruction, but fewer waves.  (300000 x 148 in f32: 84 us as waves, so 37; 8000 of them
 // 4.1 and 3.3; 8000 x 30 in f32 3.4 and 3.2, 8000 x 113 in f16 3.3 and 3.6.)  With alternatives, which cost
-// each lane its words, up to 64 words (200000 x 1000 in f16, 32 lanes or a wave: none 83 and 97, four
-// of them 193 and 156).  The gradient four times as
+// each lane its words, only up to 64 words for kFew of them and 32 for more (200000 x 1000 in f16, 32 lanes
+// or a wave: none 83 and 97, four of them 193 and 156).  The gradient four times as
 // many, where the lanes' idle words are more than the last of a line (300000 x 66 in f16: 26.7 us, so
 // 18.8; x 148 in f32 114 and 69; but x 113 in f16, fifteen of sixteen lanes, 30.0 and 34.4 to 46; 30000 x
 // 148 in f32 10.2 and 8.9; 8000 x 300 in f16 5.3 and 5.0, x 256 in f32 4.4 and 5.3).
