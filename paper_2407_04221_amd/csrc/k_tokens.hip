@@ -122,8 +122,8 @@ __device__ inline float weight_below(float l, float m) {
 }
 // A weight, or 0 for the largest's, which rows of one thread or of few lanes sum beside S: one instruction and
 // an addition an element, whatever the logits (300000 x 148 in f32: 29.3 us, without 28; only for rows that need
-// it, 28.7 where none does and 31.4 where many do; x 300 in f16 47, without 40, and 43.6 and 50.7).  One that rounds to 1 is left
-// out too, but then S is not certain().
+// it, 28.7 where none does and 31.4 where many do; x 300 in f16 47, without 40, and 43.6 and 50.7).  One
+// that rounds to 1 is left out too, but then S is not certain().
 __device__ inline float below_one(float e) { return __builtin_amdgcn_fractf(e); }
 
 // log (1 + x) for 0 <= x <= 1/2, twice the area hyperbolic tangent of z = x / (2 + x) <= 1/5: z (1 + z^2 / 3 +
