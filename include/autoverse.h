@@ -557,7 +557,7 @@ av_status av_log_probs_backward(const av_tokens_config *cfg, const void *logits,
 /* Draw one action per row from softmax(logits), for av_step: the smallest i for which
  * p_0 + .. + p_i > u, in 64 bits; the last choice that is not masked if there is none (u >= 1 or
  * NaN).  uniform: device float [N], numbers in [0, 1) from the caller's generator; actions:
- * device uint8 [N]; logp: device float [N] or NULL, the drawn action's log-probability.
+ * device uint8 [N]; logp: device float [N] or NULL, the drawn action's log-probability in 32 bits.
  * A <= 256 (an action is one byte).  A row without any choice draws 0 with logp -infinity, a row
  * holding a NaN or +infinity draws 0 with logp NaN. */
 av_status av_draw_actions(const av_tokens_config *cfg, const void *logits, const float *uniform,

@@ -801,6 +801,7 @@ hipError_t pick(const ScanArgs &a, const ScanPlan &plan, bool col, bool back, hi
             return col ? launch<T, V, kGated, true, true, false, kEach>(a, plan, s)
                        : launch<T, V, kGated, false, true, false, kEach>(a, plan, s);
     }
+    if (back) return hipErrorInvalidValue;             // no plan leads here
     return col ? launch<T, V, kGated, true, false, false, kEach>(a, plan, s)
                : launch<T, V, kGated, false, false, false, kEach>(a, plan, s);
 }
